@@ -415,6 +415,68 @@ int tide_rope(int B, int S, int n_heads, int n_kv_heads, int head_dim, float the
 int tide_ce_train(int64_t rows, int32_t vocab, void *z, int64_t ldz, const int32_t *tokens,
                   const uint8_t *mask, float *lse, float *loss_rows, int dtype, void *stream);
 
+/* The largest logits of every row, what a served target leaves of its answer for a draft to be trained on (Sec. 3.2: signals
+ * are captured while serving; k logits per position are 2 * k numbers where the whole row would be vocab):
+ * z [rows, ldz] (DEVICE, dtype TIDE_DTYPE_*, ldz a multiple of 8 and >= vocab, rows 16-byte aligned) is read;
+ *   ids    DEVICE int32 [rows, k], values DEVICE float [rows, k]: the k largest of columns [0, vocab), the largest first, equal
+ *          values (the two zeros too) by ascending column; a NaN counts as larger than every number.  Columns [vocab, ldz) may
+ *          hold anything.
+ *   lse    DEVICE float [rows] or NULL: the log-sum-exp of z / temperature (-inf for a row of -inf, +inf for one that holds +inf,
+ *          NaN for one that holds NaN and no +inf)
+ * 1 <= k <= min(vocab, 128), temperature in [1e-6, 1e6]; rows may be 0 (the arrays may be NULL then).  Enqueues one kernel and nothing else. */
+int tide_topk_logits(int64_t rows, int32_t vocab, const void *z, int64_t ldz, int32_t k, float temperature,
+                     int32_t *ids, float *values, float *lse, int dtype, void *stream);
+
+/* Distillation of a block of student logits z [rows, ldz] (as in tide_ce_train) from a teacher's top logits.  Of row r, over its
+ * entries j with 0 <= teacher_ids[r, j] < vocab (others are ignored, so that a row may have fewer than k), with
+ * a_j = teacher_logits[r, j] / temperature:
+ *     p_j  = exp(a_j - L),  L = log-sum-exp of these a_j, or teacher_lse[r] if teacher_lse is given (the log-sum-exp of the
+ *            teacher's WHOLE row over the temperature, as tide_topk_logits gives it: p_j are then the teacher's probabilities,
+ *            and what it has outside of its k entries is left out);  P = sum_j p_j
+ *     q    = softmax(z[r, 0..vocab) / temperature),  lse[r] = the log-sum-exp of z / temperature
+ *     loss_rows[r] = keep_r temperature^2 sum_j p_j (log p_j - log q[ids_j])
+ *     dz[r, c]     = keep_r temperature (P q[c] - sum of p_j with ids_j == c)   for c < vocab, 0 for c in [vocab, ldz)
+ * (the gradient of loss_rows[r]; not divided by the number of rows), keep_r = mask[r] != 0 and some entry is above -inf.  A column
+ * may occur several times among a row's entries.  Rows that are not kept get zeros whatever they hold; lse is written for every row.
+ *   teacher_ids DEVICE int32 [rows, k], teacher_logits DEVICE float [rows, k], teacher_lse DEVICE float [rows] or NULL
+ *   mask, lse, loss_rows  DEVICE [rows]
+ *   dz   DEVICE, layout and dtype of z: z itself (in place) or an array that does not overlap it
+ * tide_distill_eval gives lse and loss_rows alone and leaves z as it is.  1 <= k <= 128, temperature in [1e-6, 1e6]; rows may be 0 (the arrays
+ * may be NULL then).
+ * Each call enqueues one kernel and nothing else. */
+int tide_distill_eval(int64_t rows, int32_t vocab, const void *z, int64_t ldz, int32_t k, const int32_t *teacher_ids,
+                      const float *teacher_logits, const float *teacher_lse, float temperature, const uint8_t *mask,
+                      float *lse, float *loss_rows, int dtype, void *stream);
+int tide_distill_train(int64_t rows, int32_t vocab, const void *z, void *dz, int64_t ldz, int32_t k, const int32_t *teacher_ids,
+                       const float *teacher_logits, const float *teacher_lse, float temperature, const uint8_t *mask,
+                       float *lse, float *loss_rows, int dtype, void *stream);
+
+/* Cross-entropy of an LM head from the hidden states, z = y w^T, without keeping logits: the forward call gives
+ *     lse[r] = log-sum-exp of z[r, :],  loss_rows[r] = lse[r] - z[r, tokens[r]]       (both 0 where keep_r is 0)
+ * and the backward call, from the same y, w, tokens, mask and that lse,
+ *     dy = scale * dz w,  dw = scale * dz^T y,   dz[r, c] = keep_r row_weights[r] (exp(z[r, c] - lse[r]) - [c == tokens[r]])
+ * with keep_r = mask[r] != 0 and 0 <= tokens[r] < vocab.  Logits exist only for a piece of the vocabulary at a time (tide_ce_train's
+ * way keeps a block of rows over the whole vocabulary).  Rows that are not kept are not computed: their y may hold anything,
+ * they add nothing to dw, and their dy is 0.
+ *   y            DEVICE [rows, d], w DEVICE [vocab, d], of dtype TIDE_DTYPE_*; tokens DEVICE int32 [rows], mask DEVICE [rows]
+ *   row_weights  DEVICE float [rows] or NULL (all 1): the gradient that arrives at each loss_rows[r]; scale: a factor on all of
+ *                them (1 / number of kept rows: the gradients of the mean loss)
+ *   dy           DEVICE [rows, d] of dtype, overwritten
+ *   dw           DEVICE [vocab, d], overwritten, of dw_dtype: TIDE_DTYPE_FP32, or dtype; NULL where the head is frozen
+ *   workspace    DEVICE, 256-byte aligned, of at least tide_lm_ce_workspace_bytes(rows, vocab, d, dtype) bytes (0 = sizes the
+ *                calls refuse); the same size serves both calls, nothing in it has to survive between them, and calls that overlap
+ *                need one each.  It never falls as rows grow.
+ * rows in [1, 2^22], vocab and d in [1, 2^21); bf16: d a multiple of 8, vocab >= 8; y, w, dy and dw 16-byte aligned.
+ * dtype TIDE_DTYPE_BF16: logits and sums are fp32; dz is rounded to bf16 (it is an operand of the two products), and dy and a
+ * bf16 dw once from their fp32 sums.  Enqueues kernels on `stream` and nothing else. */
+size_t tide_lm_ce_workspace_bytes(int64_t rows, int32_t vocab, int64_t d, int dtype);
+int tide_lm_ce_fwd(int64_t rows, int32_t vocab, int64_t d, const void *y, const void *w, const int32_t *tokens,
+                   const uint8_t *mask, float *lse, float *loss_rows, int dtype,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int tide_lm_ce_bwd(int64_t rows, int32_t vocab, int64_t d, const void *y, const void *w, const int32_t *tokens,
+                   const uint8_t *mask, const float *lse, const float *row_weights, float scale, void *dy, void *dw, int dw_dtype,
+                   int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- Measurement support ----
  * Between tide_profile_start and tide_profile_stop every kernel the library
  * enqueues is bracketed by a pair of HIP events recorded on the caller's stream

@@ -119,6 +119,18 @@ _lib.tide_attention_bwd.restype = _i32
 _lib.tide_attention_bwd.argtypes = [_i32] * 5 + [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp]
 _lib.tide_ce_train.restype = _i32
 _lib.tide_ce_train.argtypes = [_i64, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _vp]
+_lib.tide_topk_logits.restype = _i32
+_lib.tide_topk_logits.argtypes = [_i64, _i32, _vp, _i64, _i32, _f32, _vp, _vp, _vp, _i32, _vp]
+_lib.tide_distill_eval.restype = _i32
+_lib.tide_distill_eval.argtypes = [_i64, _i32, _vp, _i64, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _i32, _vp]
+_lib.tide_distill_train.restype = _i32
+_lib.tide_distill_train.argtypes = [_i64, _i32, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _i32, _vp]
+_lib.tide_lm_ce_workspace_bytes.restype = _sz
+_lib.tide_lm_ce_workspace_bytes.argtypes = [_i64, _i32, _i64, _i32]
+_lib.tide_lm_ce_fwd.restype = _i32
+_lib.tide_lm_ce_fwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]
+_lib.tide_lm_ce_bwd.restype = _i32
+_lib.tide_lm_ce_bwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _i32, _i32, _vp, _sz, _vp]
 _lib.tide_rope.restype = _i32
 _lib.tide_rope.argtypes = [_i32] * 5 + [_f32, _vp, _vp, _i32, _i32, _vp]
 
@@ -137,7 +149,8 @@ EXPORTED = ("tide_last_error", "tide_draft_workspace_bytes", "tide_draft_workspa
     "tide_ingest_done", "tide_ingest_last_error", "tide_gemm_workspace_bytes", "tide_gemm",
             "tide_rmsnorm_fwd", "tide_rmsnorm_bwd_scratch_bytes", "tide_rmsnorm_bwd", "tide_rmsnorm_bwd_static",
             "tide_attention_fwd", "tide_attention_bwd", "tide_rope", "tide_ce_train", "tide_profile_start",
-            "tide_profile_stop")
+            "tide_profile_stop", "tide_topk_logits", "tide_distill_eval", "tide_distill_train", "tide_lm_ce_workspace_bytes",
+            "tide_lm_ce_fwd", "tide_lm_ce_bwd")
 
 
 def lib():
@@ -390,6 +403,47 @@ def tide_rope(B, S, nh, nkv, dh, theta, qkv, table, inverse, dtype, stream):
 
 def tide_ce_train(rows, vocab, z, ldz, tokens, mask, lse, loss_rows, dtype, stream, check=True):
     rc = _lib.tide_ce_train(int(rows), int(vocab), _ptr(z), int(ldz), _ptr(tokens), _ptr(mask), _ptr(lse), _ptr(loss_rows), dtype, stream)
+    return _check(rc) if check else rc
+
+
+def tide_topk_logits(rows, vocab, z, ldz, k, temperature, ids, values, lse, dtype, stream, check=True):
+    """lse may be None."""
+    rc = _lib.tide_topk_logits(int(rows), int(vocab), _ptr(z), int(ldz), int(k), float(temperature), _ptr(ids), _ptr(values), _ptr(lse),
+                               dtype, stream)
+    return _check(rc) if check else rc
+
+
+def tide_distill_eval(rows, vocab, z, ldz, k, teacher_ids, teacher_logits, teacher_lse, temperature, mask, lse, loss_rows, dtype, stream,
+                      check=True):
+    """teacher_lse may be None: the teacher's probabilities are then those among its k entries."""
+    rc = _lib.tide_distill_eval(int(rows), int(vocab), _ptr(z), int(ldz), int(k), _ptr(teacher_ids), _ptr(teacher_logits), _ptr(teacher_lse),
+                                float(temperature), _ptr(mask), _ptr(lse), _ptr(loss_rows), dtype, stream)
+    return _check(rc) if check else rc
+
+
+def tide_distill_train(rows, vocab, z, dz, ldz, k, teacher_ids, teacher_logits, teacher_lse, temperature, mask, lse, loss_rows, dtype, stream,
+                       check=True):
+    """tide_distill_eval with the gradient in dz, which may be z."""
+    rc = _lib.tide_distill_train(int(rows), int(vocab), _ptr(z), _ptr(dz), int(ldz), int(k), _ptr(teacher_ids), _ptr(teacher_logits),
+                                 _ptr(teacher_lse), float(temperature), _ptr(mask), _ptr(lse), _ptr(loss_rows), dtype, stream)
+    return _check(rc) if check else rc
+
+
+def tide_lm_ce_workspace_bytes(rows, vocab, d, dtype):
+    return int(_lib.tide_lm_ce_workspace_bytes(int(rows), int(vocab), int(d), dtype))
+
+
+def tide_lm_ce_fwd(rows, vocab, d, y, w, tokens, mask, lse, loss_rows, dtype, workspace, workspace_bytes, stream, check=True):
+    rc = _lib.tide_lm_ce_fwd(int(rows), int(vocab), int(d), _ptr(y), _ptr(w), _ptr(tokens), _ptr(mask), _ptr(lse), _ptr(loss_rows), dtype,
+                             _ptr(workspace), int(workspace_bytes), stream)
+    return _check(rc) if check else rc
+
+
+def tide_lm_ce_bwd(rows, vocab, d, y, w, tokens, mask, lse, row_weights, scale, dy, dw, dw_dtype, dtype, workspace, workspace_bytes, stream,
+                   check=True):
+    """row_weights and dw may be None."""
+    rc = _lib.tide_lm_ce_bwd(int(rows), int(vocab), int(d), _ptr(y), _ptr(w), _ptr(tokens), _ptr(mask), _ptr(lse), _ptr(row_weights),
+                             float(scale), _ptr(dy), _ptr(dw), dw_dtype, dtype, _ptr(workspace), int(workspace_bytes), stream)
     return _check(rc) if check else rc
 
 

@@ -137,6 +137,41 @@ hipError_t launch_ce_stats(int64_t rows, int V, const void* z, int64_t ldz, cons
 hipError_t launch_ce_train(int64_t rows, int V, void* z, int64_t ldz, const int32_t* tokens, const uint8_t* mask,
                            float* lse, float* loss_rows, const int* rows_dev, int64_t rows_off, int dtype,
                            hipStream_t s);
+// ---- distill.hip: a teacher's top logits, and the loss on them ---------------------------------------------------
+// the k largest of every row of z [rows, ldz] (value descending, equal values by ascending index; NaN first), and optionally
+// the log-sum-exp of z / tau
+hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, int k, float tau, int32_t* ids, float* values,
+                              float* lse, int dtype, hipStream_t s);
+constexpr int kMaxTeacher = 128;   // teacher logits of a row
+struct DistillArgs {
+  int64_t rows;
+  int V;
+  const void* z; void* dz;         // [rows, ldz]; dz NULL: the loss alone; dz == z: in place
+  int64_t ldz;
+  int k;
+  const int32_t* ids; const float* t; const float* tlse;   // [rows, k], [rows, k], [rows] or NULL
+  float tau;
+  const uint8_t* mask;
+  float *lse, *loss_rows;
+};
+hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s);
+
+// ---- lm_ce.hip: cross-entropy of the LM head from hidden states, without keeping logits --------------------------
+struct LmCeArgs {
+  int64_t rows, V, d;
+  const void *y, *w;               // [rows, d], [V, d]
+  const int32_t* tokens; const uint8_t* mask;
+  float *lse, *loss_rows;          // forward: written; backward: lse is read
+  const float* row_weights;        // backward, optional
+  float scale;
+  void *dy, *dw;                   // [rows, d] of dtype; [V, d] of dw_dtype, optional
+  int dw_dtype, dtype;
+  void* ws;
+};
+size_t lm_ce_workspace_bytes(int64_t rows, int64_t V, int64_t d, int dtype);
+hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s);
+hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s);
+
 // loss = scal[1] * sum of loss_rows[0 .. *cnt); optionally accuracy = scal[1] * sum of hit_rows[0 .. *cnt)
 hipError_t launch_loss_reduce(const float* loss_rows, const float* hit_rows, const int* cnt, const float* scal,
                               float* loss_out, float* acc_out, int* status, hipStream_t s);

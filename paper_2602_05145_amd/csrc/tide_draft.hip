@@ -1200,6 +1200,90 @@ int tide_ce_train(int64_t rows, int32_t vocab, void* z, int64_t ldz, const int32
   return TIDE_OK;
 }
 
+static bool logits_ok(int64_t rows, int32_t vocab, const void* z, int64_t ldz, float temperature, int dtype) {
+  if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || ldz < vocab || ldz % 8) { fail(TIDE_ERR_CONFIG, "bad logit block shape"); return false; }
+  if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
+  if (!(temperature >= 1e-6f && temperature <= 1e6f)) { fail(TIDE_ERR_CONFIG, "temperature must be in [1e-6, 1e6]"); return false; }
+  if (((uintptr_t)z) & 15) { fail(TIDE_ERR_CONFIG, "z must be 16-byte aligned"); return false; }
+  return true;
+}
+
+int tide_topk_logits(int64_t rows, int32_t vocab, const void* z, int64_t ldz, int32_t k, float temperature, int32_t* ids, float* values, float* lse,
+                     int dtype, void* stream) {
+  if (rows != 0 && (!z || !ids || !values)) return fail(TIDE_ERR_NULL, "z, ids and values must not be NULL");
+  if (!logits_ok(rows, vocab, z, ldz, temperature, dtype)) return TIDE_ERR_CONFIG;
+  if (k < 1 || k > vocab || k > kMaxTeacher) return fail(TIDE_ERR_CONFIG, "k must be in [1, min(vocab, %d)]", kMaxTeacher);
+  TIDE_HIP(launch_topk_logits(rows, vocab, z, ldz, k, temperature, ids, values, lse, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, (hipStream_t)stream), "topk logits");
+  return TIDE_OK;
+}
+
+static int distill(int64_t rows, int32_t vocab, const void* z, void* dz, int64_t ldz, int32_t k, const int32_t* teacher_ids, const float* teacher_logits,
+                   const float* teacher_lse, float temperature, const uint8_t* mask, float* lse, float* loss_rows, int dtype, void* stream) {
+  if (rows != 0 && (!z || !teacher_ids || !teacher_logits || !mask || !lse || !loss_rows)) return fail(TIDE_ERR_NULL, "NULL argument");
+  if (!logits_ok(rows, vocab, z, ldz, temperature, dtype)) return TIDE_ERR_CONFIG;
+  if (((uintptr_t)dz) & 15) return fail(TIDE_ERR_CONFIG, "dz must be 16-byte aligned");
+  if (k < 1 || k > kMaxTeacher) return fail(TIDE_ERR_CONFIG, "k must be in [1, %d]", kMaxTeacher);
+  const DistillArgs a{rows, vocab, z, dz, ldz, k, teacher_ids, teacher_logits, teacher_lse, temperature, mask, lse, loss_rows};
+  TIDE_HIP(launch_distill(a, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, (hipStream_t)stream), "distill");
+  return TIDE_OK;
+}
+
+int tide_distill_eval(int64_t rows, int32_t vocab, const void* z, int64_t ldz, int32_t k, const int32_t* teacher_ids, const float* teacher_logits,
+                      const float* teacher_lse, float temperature, const uint8_t* mask, float* lse, float* loss_rows, int dtype, void* stream) {
+  return distill(rows, vocab, z, nullptr, ldz, k, teacher_ids, teacher_logits, teacher_lse, temperature, mask, lse, loss_rows, dtype, stream);
+}
+
+int tide_distill_train(int64_t rows, int32_t vocab, const void* z, void* dz, int64_t ldz, int32_t k, const int32_t* teacher_ids,
+                       const float* teacher_logits, const float* teacher_lse, float temperature, const uint8_t* mask, float* lse, float* loss_rows,
+                       int dtype, void* stream) {
+  if (rows != 0 && !dz) return fail(TIDE_ERR_NULL, "dz is NULL");
+  return distill(rows, vocab, z, dz, ldz, k, teacher_ids, teacher_logits, teacher_lse, temperature, mask, lse, loss_rows, dtype, stream);
+}
+
+static bool lm_ce_sizes_ok(int64_t rows, int32_t vocab, int64_t d, int dtype) {
+  if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
+  if (rows < 1 || rows > ((int64_t)1 << 22) || vocab < 1 || vocab >= (1 << 21) || d < 1 || d >= (1 << 21)) {
+    fail(TIDE_ERR_CONFIG, "rows must be in [1, 2^22], vocab and d in [1, 2^21)");
+    return false;
+  }
+  if (dtype == TIDE_DTYPE_BF16 && (d % 8 || vocab < 8)) { fail(TIDE_ERR_CONFIG, "bf16: d must be a multiple of 8, and vocab at least 8"); return false; }
+  return true;
+}
+
+static int lm_ce_check(const LmCeArgs& a, const void* workspace, size_t workspace_bytes) {
+  if (!lm_ce_sizes_ok(a.rows, (int32_t)a.V, a.d, a.dtype)) return TIDE_ERR_CONFIG;
+  if (((uintptr_t)a.y | (uintptr_t)a.w | (uintptr_t)a.dy | (uintptr_t)a.dw) & 15) return fail(TIDE_ERR_CONFIG, "y, w, dy and dw must be 16-byte aligned");
+  if (((uintptr_t)workspace) & 255) return fail(TIDE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const size_t need = lm_ce_workspace_bytes(a.rows, a.V, a.d, a.dtype);
+  if (workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  return TIDE_OK;
+}
+
+size_t tide_lm_ce_workspace_bytes(int64_t rows, int32_t vocab, int64_t d, int dtype) {
+  return lm_ce_sizes_ok(rows, vocab, d, dtype) ? lm_ce_workspace_bytes(rows, vocab, d, dtype) : 0;
+}
+
+int tide_lm_ce_fwd(int64_t rows, int32_t vocab, int64_t d, const void* y, const void* w, const int32_t* tokens, const uint8_t* mask, float* lse,
+                   float* loss_rows, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!y || !w || !tokens || !mask || !lse || !loss_rows || !workspace) return fail(TIDE_ERR_NULL, "NULL argument");
+  const LmCeArgs a{rows, vocab, d, y, w, tokens, mask, lse, loss_rows, nullptr, 1.f, nullptr, nullptr, dtype, dtype, workspace};
+  if (const int rc = lm_ce_check(a, workspace, workspace_bytes)) return rc;
+  TIDE_HIP(launch_lm_ce_fwd(a, (hipStream_t)stream), "lm ce forward");
+  return TIDE_OK;
+}
+
+int tide_lm_ce_bwd(int64_t rows, int32_t vocab, int64_t d, const void* y, const void* w, const int32_t* tokens, const uint8_t* mask, const float* lse,
+                   const float* row_weights, float scale, void* dy, void* dw, int dw_dtype, int dtype, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  if (!y || !w || !tokens || !mask || !lse || !dy || !workspace) return fail(TIDE_ERR_NULL, "NULL argument");
+  if (dw && dw_dtype != TIDE_DTYPE_FP32 && dw_dtype != dtype) return fail(TIDE_ERR_CONFIG, "dw_dtype must be TIDE_DTYPE_FP32 or dtype");
+  if (!std::isfinite(scale)) return fail(TIDE_ERR_CONFIG, "scale must be finite");
+  const LmCeArgs a{rows, vocab, d, y, w, tokens, mask, const_cast<float*>(lse), nullptr, row_weights, scale, dy, dw, dw_dtype, dtype, workspace};
+  if (const int rc = lm_ce_check(a, workspace, workspace_bytes)) return rc;
+  TIDE_HIP(launch_lm_ce_bwd(a, (hipStream_t)stream), "lm ce backward");
+  return TIDE_OK;
+}
+
 }  // extern "C"
 
 // ---- optional per-launch profiler (prof.h) --------------------------------------------------------

@@ -1,0 +1,226 @@
+"""tide_distill_eval / tide_distill_train against the definition in 64 bits, and the gradient against differences."""
+import pytest
+import torch
+
+from paper_2602_05145_amd import binding as B
+from tests.gpu_util import stream, sync
+from tests.loss_util import CODE, DEV, HALF, STEP, TDT, assert_within, gen, logits, lse64, padded, sum_rel
+
+pytestmark = pytest.mark.gpu
+
+
+def teacher(rows, vocab, k, seed):
+    g = gen(seed + 50)
+    ids = torch.stack([torch.randperm(vocab, device=DEV, generator=g)[:k] if k <= vocab else torch.randint(0, vocab, (k,), device=DEV, generator=g)
+                       for _ in range(rows)]).to(torch.int32)
+    t = 3.0 * torch.randn((rows, k), device=DEV, generator=g) + 4.0
+    return ids, t
+
+
+def call(z, vocab, ids, t, tlse, tau, mask, train=True, in_place=False, guard=2):
+    rows, ldz = z.shape
+    dtype = "bf16" if z.dtype == torch.bfloat16 else "fp32"
+    lse, loss = (torch.full((rows + guard,), -7.0, device=DEV) for _ in range(2))
+    k = ids.shape[1]
+    if not train:
+        before = z.clone()
+        B.tide_distill_eval(rows, vocab, z, ldz, k, ids, t, tlse, tau, mask, lse, loss, CODE[dtype], stream())
+        sync()
+        assert torch.equal(z.view(torch.uint8), before.view(torch.uint8))
+        dz = None
+    else:
+        whole = torch.full((rows + guard, ldz), -7.0, device=DEV, dtype=z.dtype)
+        if in_place:
+            whole[:rows] = z
+        dz = whole[:rows]
+        B.tide_distill_train(rows, vocab, dz if in_place else z, dz, ldz, k, ids, t, tlse, tau, mask, lse, loss, CODE[dtype], stream())
+        sync()
+        assert bool((whole[rows:] == -7).all())
+    assert bool((lse[rows:] == -7).all()) and bool((loss[rows:] == -7).all())
+    return lse[:rows], loss[:rows], dz
+
+
+def reference(z, vocab, ids, t, tlse, tau, mask):
+    """(lse, its bound), (loss, bound), (dz, bound without the rounding of the stored result)."""
+    x = z[:, :vocab].double() / tau
+    valid = (ids >= 0) & (ids < vocab)
+    a = torch.where(valid, t.double() / tau, -torch.inf)
+    keep = (mask != 0) & (a > -torch.inf).any(1)
+    L = torch.logsumexp(a, 1) if tlse is None else tlse.double()
+    p = torch.where(valid & keep[:, None], torch.exp(a - L[:, None]), 0.0)
+    lse, lse_tol = lse64(z[:, :vocab].float(), tau)
+    log_q = x.gather(1, torch.where(valid, ids, 0).long()) - lse[:, None]
+    diff = torch.where(p > 0, a - L[:, None] - log_q, 0.0)
+    loss = torch.where(keep, tau * tau * (p * diff).sum(1), 0.0)
+    # p: the teacher's sum of up to 128 terms, exponents and quotients of numbers up to max |a|; q: the row's sum
+    reach = float(a[a.isfinite()].abs().max()) if a.isfinite().any() else 0.0
+    p_rel = (40 + 4 * reach + (0 if tlse is None else 2 * float(tlse.abs().max()))) * HALF
+    q_rel = 2 * sum_rel(vocab, float(x[x.isfinite()].abs().max()))
+    loss_tol = tau * tau * (p * ((p_rel + 130 * HALF) * (diff.abs() + 1) + lse_tol + 8 * HALF * (1 + log_q.abs().clamp(max=1e4)))).sum(1)
+    mass = p.sum(1, keepdim=True)
+    q = torch.exp(x - lse[:, None])
+    at = torch.zeros_like(q).scatter_add_(1, torch.where(valid, ids, 0).long(), p)
+    dz = torch.where(keep[:, None], tau * (mass * q - at), 0.0)
+    dz_tol = tau * (mass * q * (q_rel + p_rel + 140 * HALF) + at * (p_rel + 130 * HALF)) + 1e-37
+    return (lse, lse_tol), (loss, loss_tol), (dz, dz_tol)
+
+
+def check(z, vocab, ids, t, tlse, tau, mask, train=True):
+    dtype = "bf16" if z.dtype == torch.bfloat16 else "fp32"
+    (lse, lse_tol), (loss, loss_tol), (dz, dz_tol) = reference(z, vocab, ids, t, tlse, tau, mask)
+    outs = [call(z, vocab, ids, t, tlse, tau, mask, train=False)]
+    if train:
+        outs += [call(z, vocab, ids, t, tlse, tau, mask), call(z, vocab, ids, t, tlse, tau, mask, in_place=True)]
+        assert torch.equal(outs[1][2].view(torch.uint8), outs[2][2].view(torch.uint8))
+    for got_lse, got_loss, got_dz in outs:
+        assert_within(got_lse, lse, lse_tol, "lse")
+        assert_within(got_loss, loss, loss_tol, "loss")
+        if got_dz is not None:
+            assert bool((got_dz[:, vocab:] == 0).all())
+            assert_within(got_dz[:, :vocab], dz, dz_tol + (dz.abs() + dz_tol) * STEP[dtype], "dz")
+
+
+SHAPES = [(1, 8, 0, 1, 1.0), (1, 1, 0, 1, 1.0), (2, 5, 8, 3, 2.0), (3, 100, 0, 100, 0.5), (5, 1000, 64, 128, 1.0), (4, 4095, 0, 16, 1.0), (3, 4096, 8, 7, 1.0),
+          (2, 8193, 0, 31, 3.0), (115, 4096, 0, 16, 1.0), (5, 32001, 0, 64, 1.5), (3, 50000, 0, 20, 1.0), (9, 98304, 0, 32, 1.0), (7, 128256, 0, 32, 2.0),
+          (2, 152064, 0, 128, 1.0), (2, 175003, 0, 8, 1.0)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("given", [False, True], ids=["among k", "teacher_lse"])
+@pytest.mark.parametrize("rows,vocab,extra,k,tau", SHAPES)
+def test_against_64_bits(dtype, given, rows, vocab, extra, k, tau):
+    z = logits(rows, vocab, padded(vocab, extra), dtype, seed=vocab + k)
+    ids, t = teacher(rows, vocab, k, seed=vocab)
+    tlse = torch.logsumexp(t / tau, 1) + 0.4 if given else None
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    mask[1::3] = 0
+    check(z, vocab, ids, t, tlse, tau, mask)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [300, 9001, 128256])
+def test_entries_that_are_missing_repeated_or_empty(dtype, vocab):
+    rows, k = 9, 12
+    z = logits(rows, vocab, padded(vocab), dtype, 7)
+    ids, t = teacher(rows, vocab, k, 8)
+    ids[0, 3:] = -1                        # three entries
+    ids[1] = -1                            # none: the row is left out
+    ids[2, ::2] = vocab                    # outside
+    ids[2, 1] = 2 ** 31 - 1
+    ids[3] = ids[3, 0]                     # one column, all of the mass
+    ids[4, 1] = ids[4, 0]
+    ids[4, 7] = ids[4, 0]
+    t[5, 2:] = -float("inf")
+    t[6] = -float("inf")                   # says nothing: left out
+    ids[7] = torch.arange(vocab - k, vocab, device=DEV)   # the row's last columns
+    ids[8] = torch.arange(k, device=DEV) * 8 % vocab
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    for tlse in (None, torch.where(t.isfinite().any(1), torch.logsumexp(t, 1), 0.0) + 0.2):
+        check(z, vocab, ids, t, tlse, 1.0, mask)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [700, 33000])
+def test_rows_without_loss_may_hold_anything(dtype, vocab):
+    rows, k = 6, 5
+    z = logits(rows, vocab, padded(vocab), dtype, 9)
+    ids, t = teacher(rows, vocab, k, 10)
+    z[1] = float("nan")
+    z[2, :] = float("inf")
+    z[3] = -float("inf")
+    t[1] = float("nan")
+    t[2] = float("inf")
+    ids[1] = -2 ** 31
+    mask = torch.tensor([1, 0, 0, 0, 1, 255], dtype=torch.uint8, device=DEV)
+    lse, loss, dz = call(z, vocab, ids, t, None, 1.0, mask)
+    assert bool((loss[1:4] == 0).all()) and bool((dz[1:4] == 0).all())
+    rest = [0, 4, 5]
+    check(z[rest].contiguous(), vocab, ids[rest].contiguous(), t[rest].contiguous(), None, 1.0, mask[rest].contiguous())
+    assert lse[1].isnan() and lse[2] == float("inf") and lse[3] == -float("inf")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_masked_columns_and_confident_rows(dtype):
+    """-inf and the type's lowest value as masks of columns; a teacher entry on a column that the student excludes costs +inf."""
+    vocab, k = 5000, 6
+    low = torch.finfo(TDT[dtype]).min
+    z = logits(5, vocab, padded(vocab), dtype, 11)
+    ids, t = teacher(5, vocab, k, 12)
+    z[0, :vocab // 2] = -float("inf")
+    ids[0] += vocab // 2 - ids[0].min()
+    ids[0] = ids[0] % (vocab - vocab // 2) + vocab // 2
+    z[1, 100:4000] = low
+    ids[1] = torch.arange(k, device=DEV)
+    z[2, :vocab] = low
+    z[2, 17] = 5.0
+    ids[2] = 17
+    z[3, 9] = 60.0
+    ids[3, 0] = 9
+    z[4, 30] = -float("inf")
+    ids[4, 0] = 30
+    mask = torch.ones(5, dtype=torch.uint8, device=DEV)
+    check(z, vocab, ids, t, None, 1.0, mask)
+    assert call(z, vocab, ids, t, None, 1.0, mask)[1][4] == float("inf")
+
+
+def test_gradient_against_differences():
+    """Central differences of the loss in 64 bits: their own error is h^2 times a third derivative below 1, and rounding / h."""
+    rows, vocab, k, tau, h = 2, 24, 6, 1.7, 1e-4
+    z = logits(rows, vocab, 24, "fp32", 13)
+    ids, t = teacher(rows, vocab, k, 14)
+    ids[1, 2] = ids[1, 0]
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    for tlse in (None, torch.logsumexp(t / tau, 1) + 0.5):
+        dz = call(z, vocab, ids, t, tlse, tau, mask)[2].double()
+
+        def loss(x):
+            log_q = torch.log_softmax(x / tau, 1).gather(1, ids.long())
+            log_p = t.double() / tau - (torch.logsumexp(t.double() / tau, 1) if tlse is None else tlse.double())[:, None]
+            return tau * tau * (log_p.exp() * (log_p - log_q)).sum(1)
+
+        for c in range(vocab):
+            e = torch.zeros((1, vocab), dtype=torch.float64, device=DEV)
+            e[0, c] = h
+            d = (loss(z.double() + e) - loss(z.double() - e)) / (2 * h)
+            assert float((d - dz[:, c]).abs().max()) < 1e-5
+
+
+def test_one_teacher_token_is_the_hard_label():
+    """With one entry p = 1: the same loss and gradient as the cross-entropy pass over emitted tokens."""
+    rows, vocab = 300, 32000
+    z = logits(rows, vocab, vocab, "bf16", 15)
+    tokens = torch.randint(0, vocab, (rows,), device=DEV, generator=gen(16)).to(torch.int32)
+    tokens[5], tokens[6] = -1, vocab
+    mask = (torch.rand(rows, device=DEV, generator=gen(17)) < 0.8).to(torch.uint8)
+    lse, loss, dz = call(z, vocab, tokens[:, None].contiguous(), torch.full((rows, 1), 2.5, device=DEV), None, 1.0, mask)
+    z2, lse2, loss2 = z.clone(), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    B.tide_ce_train(rows, vocab, z2, vocab, tokens, mask, lse2, loss2, CODE["bf16"], stream())
+    sync()
+    tol = lse64(z.float(), 1.0)[1]
+    assert_within(lse, lse2, 2 * tol, "lse")
+    assert_within(loss, loss2, 2 * tol + 1e-5, "loss")
+    # each side within half a step, and two fp32 errors, of the same number: at most one step of the other
+    assert_within(dz, z2, z2.double().abs() * 2 * STEP["bf16"] * 1.01 + 1e-37, "dz")
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 17000), ("fp32", 8600)])
+def test_offsets_beyond_32_bits(dtype, rows):
+    vocab = ldz = 128256
+    z = torch.zeros((rows, ldz), device=DEV, dtype=TDT[dtype])
+    z[-1] = torch.randn(ldz, device=DEV, generator=gen(5)).to(TDT[dtype])
+    last = z[-1:].clone()
+    ids, t = teacher(1, vocab, 4, 18)
+    ids, t = ids.expand(rows, 4).contiguous(), t.expand(rows, 4).contiguous()
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    lse, loss = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    B.tide_distill_train(rows, vocab, z, z, ldz, 4, ids, t, None, 1.0, mask, lse, loss, CODE[dtype], stream())
+    sync()
+    one = call(last, vocab, ids[:1], t[:1], None, 1.0, mask[:1])
+    assert torch.equal(z[-1:], one[2]) and lse[-1] == one[0][0] and loss[-1] == one[1][0]
+    assert torch.equal(z[0], z[rows // 2])
+
+
+def test_no_rows():
+    z = logits(2, 64, 64, "fp32", 1)
+    ids, t = teacher(2, 64, 3, 1)
+    call(z[:0], 64, ids[:0], t[:0], None, 1.0, torch.ones(0, dtype=torch.uint8, device=DEV))
