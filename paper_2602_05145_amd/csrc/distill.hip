@@ -80,47 +80,257 @@ __device__ __forceinline__ float row_lse(const Online& o, float tau) {
 }  // namespace
 
 // ----------------------------------------------------------------------------------------------
-// One block per row: the log-sum-exp, then the k largest one after the other, each the largest pair below the last.
+// The k largest logits of a row and its log-sum-exp, in one read of the row.
+//
+// A block walks its row in rounds of NT x U chunks of eight columns.  What it remembers are chunks, by (largest value, index):
+// an element of the k largest lies in one of the k first chunks in that order, because any chunk before its own holds an
+// element before it (larger, or as large with a smaller index).  A threshold T that k chunks reach keeps almost every
+// chunk out after a comparison with its maximum, which is taken anyway; the others go to a list in LDS, and when that holds
+// more than k + 64 of them, a wave finds the k-th largest key bit by bit (a ballot per 64 keys and bit), which is the new T, and
+// drops the rest.  Rows of random order pass about k chunks per doubling of what has been seen.  The order of a row
+// can fill a round, never the list: it has room for one.  At the end the eight elements of each chunk left are read again
+// (a few hundred of 128256) and ranked by counting.
+// Sum of exponentials: against a shift that a wave keeps to itself and raises only where a chunk passes T (it is never below
+// T, so what does not pass cannot exceed it): per element one conversion, half a maximum, one fused step, the exponential and
+// one addition.  The first round has no T yet: each wave takes the k-th largest of its own 64 U chunk maxima, and the
+// largest of those serves all.
+// Bound by memory: [8192, 128256] bf16, k = 32: @TOPK_8B@.
 // ----------------------------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
-                                                          int32_t* __restrict__ ids, float* __restrict__ values,
-                                                          float* __restrict__ lse) {
-  __shared__ Online sm[4];
-  __shared__ uint64_t best[4];
+namespace {
+
+__device__ __forceinline__ void lds_barrier() {   // orders LDS only: loads of the next round stay in flight
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+// largest of eight, NaN if one is NaN
+__device__ __forceinline__ float max8(const float (&v)[8]) {
+  auto max3 = [](float a, float b, float c) {
+    float r;
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+  };
+  const float m = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), v[6]);
+  return max3(m, v[7], v[7]);
+}
+template <typename T> struct Raw8Once : Raw8<T> {   // loads past the caches: nothing is read again
+  __device__ __forceinline__ void load_once(const T* p, size_t i) {
+    typedef unsigned u32x4_nt __attribute__((ext_vector_type(4)));
+    const u32x4_nt* q = reinterpret_cast<const u32x4_nt*>(p + i);
+    if constexpr (sizeof(T) == 2) {
+      const u32x4_nt x = __builtin_nontemporal_load(q);
+      this->a = make_uint4(x.x, x.y, x.z, x.w);
+    } else {
+      const u32x4_nt x = __builtin_nontemporal_load(q), y = __builtin_nontemporal_load(q + 1);
+      this->a = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+      this->b = make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w));
+    }
+  }
+};
+
+constexpr int kListSlack = 64, kListKept = kMaxTeacher + kListSlack;   // chunks that a list may hold at the start of a round
+
+// By one wave, on the n > k pairs of a list: the largest 16-bit prefix that the keys of k of them reach, as a key (the whole k-th pair
+// where too many share that prefix).  Pairs below it leave the list; returns what is left, at most k + kListSlack.
+struct ListCut { int n; uint32_t key; };
+template <int NI>
+__device__ __forceinline__ uint32_t cut_prefix(const uint64_t* list, int n, int k, int lane, int& left) {
+  uint32_t key[NI];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) key[i] = lane + 64 * i < n ? (uint32_t)(list[lane + 64 * i] >> 32) : 0u;
+  uint32_t t = 0;
+  left = n;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t u = t | (1u << bit);
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) c += __popcll(__ballot(key[i] >= u));
+    if (c >= k) { t = u; left = c; }
+  }
+  return t;
+}
+__device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int lane) {
+  int left = n;
+  uint64_t t;
+  if (n <= 256) {
+    t = (uint64_t)cut_prefix<4>(list, n, k, lane, left) << 32;
+  } else {
+    t = 0;
+    for (int bit = 63; bit >= 48; --bit) {
+      const uint64_t u = t | (1ull << bit);
+      int c = 0;
+      for (int i = 0; i < n; i += 64) c += __popcll(__ballot(i + lane < n && list[i + lane] >= u));
+      if (c >= k) { t = u; left = c; }
+    }
+  }
+  const uint32_t key = (uint32_t)(t >> 32);
+  if (left > k + kListSlack)
+    for (int bit = 47; bit >= 0; --bit) {
+      const uint64_t u = t | (1ull << bit);
+      int c = 0;
+      for (int i = 0; i < n; i += 64) c += __popcll(__ballot(i + lane < n && list[i + lane] >= u));
+      if (c >= k) t = u;
+    }
+  int out = 0;
+  for (int i = 0; i < n; i += 64) {   // (a pair moves down or stays: what is written has been read)
+    const uint64_t p = i + lane < n ? list[i + lane] : 0;
+    const uint64_t kept = __ballot(i + lane < n && p >= t);
+    if (i + lane < n && p >= t) list[out + __popcll(kept & ((1ull << lane) - 1))] = p;
+    out += __popcll(kept);
+  }
+  return ListCut{out, key};
+}
+
+}  // namespace
+
+template <typename T, int NT, int U>
+__global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
+                                                         int32_t* __restrict__ ids, float* __restrict__ values,
+                                                         float* __restrict__ lse) {
+  constexpr int NW = NT / 64, ROUND = NT * U * 8;
+  constexpr int CAP = NT * U + kListKept > kListKept * 8 ? NT * U + kListKept : kListKept * 8;
+  __shared__ uint64_t list[CAP];
+  __shared__ uint32_t chunk_of[kListKept];
+  __shared__ int added[3];
+  __shared__ uint32_t first_key, cut_key, top_key;
+  __shared__ int cut_n, found_n;
+  __shared__ Online sm[NW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const size_t row = blockIdx.x;
   const T* zr = z + row * (size_t)ldz;
   const float c = kLog2e / tau;
-  if (lse) {
-    Online o{-INFINITY, 0.f};
-    for (int i = threadIdx.x * 8; i < V; i += 256 * 8) {
-      float v[8];
-      load_tail8(zr, i, V, v);
-      online_add8(o, v, c);
+  const int last = (V - 1) / 8 * 8;                 // the last chunk: whole in memory, since rows are multiples of eight apart
+  if (threadIdx.x < 3) added[threadIdx.x] = 0;
+  if (threadIdx.x == 3) { first_key = 0; found_n = 0; }
+  lds_barrier();
+
+  Raw8Once<T> cur[U], nxt[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) cur[u].load_once(zr, (size_t)min((int)(threadIdx.x + u * NT) * 8, last));
+  int n = 0;                                        // pairs in the list
+  float T_v = __uint_as_float(0x7FC00000u);         // chunks pass unless their maximum is at most this: all, so far
+  float m = -INFINITY, s = 0.f;                     // the wave's shift, the lane's sum
+  float shift = 0.f;                                // -c m, 0 before any number
+  bool wide = false;                                // whether that is too large to be added to
+  auto raise = [&](float to) {                      // the same in the whole wave
+    to = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(to)));
+    if (to > m) {
+      s *= m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);   // (before any number the sum is 0, or NaN)
+      m = to;
+      shift = -m * c;
+      wide = !(fabsf(shift) < 1e30f);
     }
-    o = online_block<256>(o, c, sm);
-    if (threadIdx.x == 0) lse[row] = row_lse(o, tau);
-  }
-  uint64_t last = ~0ull;
-  for (int j = 0; j < k; ++j) {
-    uint64_t mine = 0;
-    for (int i = threadIdx.x; i < V; i += 256) {
-      const uint64_t p = order_pair(ldf(zr, i), i);
-      if (p < last && p > mine) mine = p;
+  };
+  auto columns = [&](const Raw8Once<T>& raw, int col, bool tail, float (&v)[8]) {
+    raw.get(v);
+    if (tail) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = col + j < V ? v[j] : -INFINITY;
+    }
+  };
+  for (int base = 0, r = 0; base < V; base += ROUND, r = r == 2 ? 0 : r + 1) {
+    const bool tail = base + ROUND > V;
+    if (base + ROUND < V) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) nxt[u].load_once(zr, (size_t)min(base + ROUND + (int)(threadIdx.x + u * NT) * 8, last));
+    }
+    if (base == 0) {
+      uint32_t key[U];
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int col = (threadIdx.x + u * NT) * 8;
+        float v[8];
+        columns(cur[u], col, tail, v);
+        const float cm = max8(v);
+        key[u] = col < V ? order_key(cm) : 0u;
+        top = fmaxf(top, cm);
+      }
+      uint32_t t = 0;
+      for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t x = t | (1u << bit);
+        int count = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) count += __popcll(__ballot(key[u] >= x));
+        if (count >= k) t = x;
+      }
+      if (lane == 0 && t) atomicMax(&first_key, t);
+      raise(wave_max(top));
+      lds_barrier();
+      t = first_key;
+      if (t > 2) T_v = key_value(t - 2);            // k chunks have keys of at least t; two steps, for the two zeros
+      raise(T_v);
     }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-      const uint64_t x = __shfl_xor((unsigned long long)mine, d, 64);
-      mine = x > mine ? x : mine;
+    for (int u = 0; u < U; ++u) {
+      const int col = base + (threadIdx.x + u * NT) * 8;
+      float v[8];
+      columns(cur[u], col, tail, v);
+      const float cm = max8(v);
+      const bool pass = col < V && !(cm <= T_v);
+      const uint64_t who = __ballot(pass);
+      if (who) {
+        raise(wave_max(fmaxf(cm, m)));
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&added[r], __popcll(who));
+        at = n + __builtin_amdgcn_readfirstlane(at);
+        if (pass) list[at + __popcll(who & ((1ull << lane) - 1))] = ((uint64_t)order_key(cm) << 32) | (uint32_t)~(col >> 3);
+      }
+      float part = 0.f;
+      if (wide) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f((v[j] - m) * c);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f(fmaf(v[j], c, shift));
+      }
+      s += part;
     }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) best[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    last = best[0];
-    for (int i = 1; i < 4; ++i) last = best[i] > last ? best[i] : last;
+    lds_barrier();
+    n += added[r];
+    if (threadIdx.x == 0) added[r == 0 ? 2 : r - 1] = 0;   // read by all before this barrier, used again behind the next
+    if (n > k + kListSlack || (base + ROUND >= V && n > k)) {
+      if (wave == 0) {
+        const ListCut cut = list_cut(list, n, k, lane);
+        if (lane == 0) { cut_n = cut.n; cut_key = cut.key; }
+      }
+      lds_barrier();
+      n = cut_n;
+      T_v = key_value(cut_key);
+      raise(T_v);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) cur[u] = nxt[u];
+  }
+
+  // the elements of the chunks left, of which k reach the last threshold
+  const uint32_t least = n >= k && T_v == T_v ? order_key(T_v) : 0u;
+  if (threadIdx.x < n) chunk_of[threadIdx.x] = ~(uint32_t)list[threadIdx.x];
+  lds_barrier();
+  for (int e = threadIdx.x; e < n * 8; e += NT) {
+    const int col = (int)(chunk_of[e >> 3] * 8u) + (e & 7);
+    if (col < V) {
+      const uint64_t p = order_pair(ldf(zr, (size_t)col), col);
+      if ((uint32_t)(p >> 32) >= least) list[atomicAdd(&found_n, 1)] = p;
+    }
+  }
+  lds_barrier();
+  const int found = found_n;
+  for (int i = threadIdx.x; i < found; i += NT) {
+    const uint64_t p = list[i];
+    int rank = 0;
+    for (int j = 0; j < found; ++j) rank += list[j] > p ? 1 : 0;
+    if (rank < k) {
+      ids[row * (size_t)k + rank] = (int32_t)~(uint32_t)p;
+      values[row * (size_t)k + rank] = key_value((uint32_t)(p >> 32));
+      if (rank == 0) top_key = (uint32_t)(p >> 32);
+    }
+  }
+  if (lse) {
+    const Online o = online_block<NT>(Online{m, s}, c, sm);
     if (threadIdx.x == 0) {
-      ids[row * (size_t)k + j] = (int32_t)~(uint32_t)last;
-      values[row * (size_t)k + j] = key_value((uint32_t)(last >> 32));
+      const float top = key_value(top_key);         // -inf, +inf and NaN have no sum: the row's log-sum-exp is its largest element
+      lse[row] = fabsf(top) < INFINITY ? o.m / tau + logf(o.s) : top;
     }
   }
 }
@@ -129,9 +339,17 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
                               int dtype, hipStream_t s) {
   if (rows <= 0) return hipSuccess;
   ProfScope ps("topk_logits", 0, (double)rows * ((double)V * dtype_size(dtype) + 8.0 * k), s);
-  const dim3 grid((unsigned)rows), blk(256);
-  if (dtype == kBF16) hipLaunchKernelGGL(topk_logits_kernel<bf16_t>, grid, blk, 0, s, (const bf16_t*)z, ldz, V, k, tau, ids, values, lse);
-  else hipLaunchKernelGGL(topk_logits_kernel<float>, grid, blk, 0, s, (const float*)z, ldz, V, k, tau, ids, values, lse);
+  const dim3 grid((unsigned)rows);
+  const bool few = rows <= 512;
+#define TIDE_TOPK(T, NT, U) hipLaunchKernelGGL((topk_logits_kernel<T, NT, U>), grid, dim3(NT), 0, s, (const T*)z, ldz, V, k, tau, ids, values, lse)
+  if (dtype == kBF16) {
+    if (few) TIDE_TOPK(bf16_t, 1024, 4);
+    else TIDE_TOPK(bf16_t, 256, 4);
+  } else {
+    if (few) TIDE_TOPK(float, 1024, 2);
+    else TIDE_TOPK(float, 256, 2);
+  }
+#undef TIDE_TOPK
   return hipGetLastError();
 }
 
