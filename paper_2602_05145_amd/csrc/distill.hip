@@ -86,7 +86,7 @@ __device__ __forceinline__ float row_lse(const Online& o, float tau) {
 // an element of the k largest lies in one of the k first chunks in that order, because any chunk before its own holds an
 // element before it (larger, or as large with a smaller index).  A threshold T that k chunks reach keeps almost every
 // chunk out after a comparison with its maximum, which is taken anyway; the others go to a list in LDS, and when that holds
-// more than k + 64 of them, a wave finds the k-th largest key bit by bit (a ballot per 64 keys and bit), which is the new T, and
+// more than k + 16 + k / 4 of them, a wave finds the k-th largest key bit by bit (a ballot per 64 keys and bit), which is the new T, and
 // drops the rest.  Rows of random order pass about k chunks per doubling of what has been seen.  The order of a row
 // can fill a round, never the list: it has room for one.  At the end the eight elements of each chunk left are read again
 // (a few hundred of 128256) and ranked by counting.
@@ -94,7 +94,7 @@ __device__ __forceinline__ float row_lse(const Online& o, float tau) {
 // T, so what does not pass cannot exceed it): per element one conversion, half a maximum, one fused step, the exponential and
 // one addition.  The first round has no T yet: each wave takes the k-th largest of its own 64 U chunk maxima, and the
 // largest of those serves all.
-// Bound by memory: [8192, 128256] bf16, k = 32: @TOPK_8B@.
+// Bound by memory: [8192, 128256] bf16, k = 32: 327 us, 6.4 TB/s (k = 1: 321, k = 128: 365).
 // ----------------------------------------------------------------------------------------------
 namespace {
 
@@ -128,10 +128,12 @@ template <typename T> struct Raw8Once : Raw8<T> {   // loads past the caches: no
   }
 };
 
-constexpr int kListSlack = 64, kListKept = kMaxTeacher + kListSlack;   // chunks that a list may hold at the start of a round
+// chunks that a list may hold at the start of a round beyond the k that it needs
+__host__ __device__ constexpr int list_slack(int k) { return 16 + k / 4; }
+constexpr int kListKept = kMaxTeacher + list_slack(kMaxTeacher);
 
 // By one wave, on the n > k pairs of a list: the largest 16-bit prefix that the keys of k of them reach, as a key (the whole k-th pair
-// where too many share that prefix).  Pairs below it leave the list; returns what is left, at most k + kListSlack.
+// where too many share that prefix).  Pairs below it leave the list; returns what is left, at most k + list_slack(k).
 struct ListCut { int n; uint32_t key; };
 template <int NI>
 __device__ __forceinline__ uint32_t cut_prefix(const uint64_t* list, int n, int k, int lane, int& left) {
@@ -152,8 +154,14 @@ __device__ __forceinline__ uint32_t cut_prefix(const uint64_t* list, int n, int 
 __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int lane) {
   int left = n;
   uint64_t t;
-  if (n <= 256) {
+  if (n <= 128) {
+    t = (uint64_t)cut_prefix<2>(list, n, k, lane, left) << 32;
+  } else if (n <= 256) {
     t = (uint64_t)cut_prefix<4>(list, n, k, lane, left) << 32;
+  } else if (n <= 512) {
+    t = (uint64_t)cut_prefix<8>(list, n, k, lane, left) << 32;
+  } else if (n <= 1024) {
+    t = (uint64_t)cut_prefix<16>(list, n, k, lane, left) << 32;
   } else {
     t = 0;
     for (int bit = 63; bit >= 48; --bit) {
@@ -164,7 +172,7 @@ __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int la
     }
   }
   const uint32_t key = (uint32_t)(t >> 32);
-  if (left > k + kListSlack)
+  if (left > k + list_slack(k))
     for (int bit = 47; bit >= 0; --bit) {
       const uint64_t u = t | (1ull << bit);
       int c = 0;
@@ -183,8 +191,9 @@ __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int la
 
 }  // namespace
 
-template <typename T, int NT, int U>
-__global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
+// (256 threads in 89 registers, five blocks on a CU: 365 us where seven take 327)
+template <typename T, int NT, int U, int D>
+__global__ __launch_bounds__(NT, NT == 256 ? 7 : 4) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
                                                          int32_t* __restrict__ ids, float* __restrict__ values,
                                                          float* __restrict__ lse) {
   constexpr int NW = NT / 64, ROUND = NT * U * 8;
@@ -204,9 +213,15 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
   if (threadIdx.x == 3) { first_key = 0; found_n = 0; }
   lds_barrier();
 
-  Raw8Once<T> cur[U], nxt[U];
+  Raw8Once<T> ring[D][U];                           // the next D rounds
+  auto load = [&](Raw8Once<T> (&raw)[U], int base) {
+    if (base < V) {
 #pragma unroll
-  for (int u = 0; u < U; ++u) cur[u].load_once(zr, (size_t)min((int)(threadIdx.x + u * NT) * 8, last));
+      for (int u = 0; u < U; ++u) raw[u].load_once(zr, (size_t)min(base + (int)(threadIdx.x + u * NT) * 8, last));
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d) load(ring[d], d * ROUND);
   int n = 0;                                        // pairs in the list
   float T_v = __uint_as_float(0x7FC00000u);         // chunks pass unless their maximum is at most this: all, so far
   float m = -INFINITY, s = 0.f;                     // the wave's shift, the lane's sum
@@ -228,15 +243,12 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
       for (int j = 0; j < 8; ++j) v[j] = col + j < V ? v[j] : -INFINITY;
     }
   };
-  for (int base = 0, r = 0; base < V; base += ROUND, r = r == 2 ? 0 : r + 1) {
+  int r = 0;                                        // the round, modulo 3
+  auto round = [&](Raw8Once<T> (&cur)[U], int base) {
     const bool tail = base + ROUND > V;
-    if (base + ROUND < V) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) nxt[u].load_once(zr, (size_t)min(base + ROUND + (int)(threadIdx.x + u * NT) * 8, last));
-    }
     if (base == 0) {
       uint32_t key[U];
-      float top = -INFINITY;
+      float all = -INFINITY;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int col = (threadIdx.x + u * NT) * 8;
@@ -244,7 +256,7 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
         columns(cur[u], col, tail, v);
         const float cm = max8(v);
         key[u] = col < V ? order_key(cm) : 0u;
-        top = fmaxf(top, cm);
+        all = fmaxf(all, cm);
       }
       uint32_t t = 0;
       for (int bit = 31; bit >= 16; --bit) {
@@ -255,12 +267,14 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
         if (count >= k) t = x;
       }
       if (lane == 0 && t) atomicMax(&first_key, t);
-      raise(wave_max(top));
+      raise(wave_max(all));
       lds_barrier();
       t = first_key;
       if (t > 2) T_v = key_value(t - 2);            // k chunks have keys of at least t; two steps, for the two zeros
       raise(T_v);
     }
+    uint64_t who[U];
+    float top[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int col = base + (threadIdx.x + u * NT) * 8;
@@ -268,14 +282,9 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
       columns(cur[u], col, tail, v);
       const float cm = max8(v);
       const bool pass = col < V && !(cm <= T_v);
-      const uint64_t who = __ballot(pass);
-      if (who) {
-        raise(wave_max(fmaxf(cm, m)));
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&added[r], __popcll(who));
-        at = n + __builtin_amdgcn_readfirstlane(at);
-        if (pass) list[at + __popcll(who & ((1ull << lane) - 1))] = ((uint64_t)order_key(cm) << 32) | (uint32_t)~(col >> 3);
-      }
+      who[u] = __ballot(pass);
+      top[u] = cm;
+      if (who[u] && __any(cm > m)) raise(wave_max(fmaxf(cm, m)));
       float part = 0.f;
       if (wide) {
 #pragma unroll
@@ -286,10 +295,24 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
       }
       s += part;
     }
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mine += __popcll(who[u]);
+    if (mine) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&added[r], mine);
+      at = n + __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if ((who[u] >> lane) & 1)
+          list[at + __popcll(who[u] & ((1ull << lane) - 1))] = ((uint64_t)order_key(top[u]) << 32) | (uint32_t)~((base >> 3) + threadIdx.x + u * NT);
+        at += __popcll(who[u]);
+      }
+    }
     lds_barrier();
     n += added[r];
     if (threadIdx.x == 0) added[r == 0 ? 2 : r - 1] = 0;   // read by all before this barrier, used again behind the next
-    if (n > k + kListSlack || (base + ROUND >= V && n > k)) {
+    if (n > k + list_slack(k) || (base + ROUND >= V && n > k)) {
       if (wave == 0) {
         const ListCut cut = list_cut(list, n, k, lane);
         if (lane == 0) { cut_n = cut.n; cut_key = cut.key; }
@@ -299,8 +322,13 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
       T_v = key_value(cut_key);
       raise(T_v);
     }
+    r = r == 2 ? 0 : r + 1;
+    load(cur, base + D * ROUND);
+  };
+  for (int base = 0; base < V; base += D * ROUND) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) cur[u] = nxt[u];
+    for (int d = 0; d < D; ++d)
+      if (base + d * ROUND < V) round(ring[d], base + d * ROUND);
   }
 
   // the elements of the chunks left, of which k reach the last threshold
@@ -319,6 +347,7 @@ __global__ __launch_bounds__(NT) void topk_logits_kernel(const T* __restrict__ z
   for (int i = threadIdx.x; i < found; i += NT) {
     const uint64_t p = list[i];
     int rank = 0;
+#pragma unroll 4
     for (int j = 0; j < found; ++j) rank += list[j] > p ? 1 : 0;
     if (rank < k) {
       ids[row * (size_t)k + rank] = (int32_t)~(uint32_t)p;
@@ -340,14 +369,19 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
   if (rows <= 0) return hipSuccess;
   ProfScope ps("topk_logits", 0, (double)rows * ((double)V * dtype_size(dtype) + 8.0 * k), s);
   const dim3 grid((unsigned)rows);
-  const bool few = rows <= 512;
-#define TIDE_TOPK(T, NT, U) hipLaunchKernelGGL((topk_logits_kernel<T, NT, U>), grid, dim3(NT), 0, s, (const T*)z, ldz, V, k, tau, ids, values, lse)
+  // Up to a row per CU, all of a CU's threads on it, and four rounds requested at a time; two rows, half of them; beyond, four waves a row
+  // (us, 1024 / 512 / 256 threads, [rows, 128256] bf16, k = 32: 61 rows 27 / 29 / 43, 256 30 / 32 / 44, 512 57 / 39 / 49,
+  // 1024 108 / 72 / 59).
+  const int nt = rows <= 256 ? 1024 : rows <= 512 ? 512 : 256;
+#define TIDE_TOPK(T, NT, U, D) hipLaunchKernelGGL((topk_logits_kernel<T, NT, U, D>), grid, dim3(NT), 0, s, (const T*)z, ldz, V, k, tau, ids, values, lse)
   if (dtype == kBF16) {
-    if (few) TIDE_TOPK(bf16_t, 1024, 4);
-    else TIDE_TOPK(bf16_t, 256, 4);
+    if (nt == 1024) TIDE_TOPK(bf16_t, 1024, 4, 4);
+    else if (nt == 512) TIDE_TOPK(bf16_t, 512, 4, 2);
+    else TIDE_TOPK(bf16_t, 256, 4, 2);
   } else {
-    if (few) TIDE_TOPK(float, 1024, 2);
-    else TIDE_TOPK(float, 256, 2);
+    if (nt == 1024) TIDE_TOPK(float, 1024, 2, 4);
+    else if (nt == 512) TIDE_TOPK(float, 512, 2, 2);
+    else TIDE_TOPK(float, 256, 2, 2);
   }
 #undef TIDE_TOPK
   return hipGetLastError();
