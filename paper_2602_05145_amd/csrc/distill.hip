@@ -62,14 +62,17 @@ __device__ __forceinline__ Online online_block(Online o, float c, Online* sm) {
   for (int i = 1; i < NT / 64; ++i) o = online_join(o, sm[i], c);
   return o;
 }
-template <typename T>
-__device__ __forceinline__ void load_tail8(const T* zr, int c, int V, float (&v)[8]) {
-  if (c + 8 <= V) {
-    ld8(zr, c, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < V ? ldf(zr, c + j) : -INFINITY;
-  }
+// 2^(c (z - m)) of values z <= m as 2^(slope z + shift), in one fused step.  Where c m is so large that 1 beside it is nothing (or it has
+// no number: columns masked with the type's lowest value), a power of two takes the place of c, so that slope m is exact, the
+// largest value still gives 1, and the next smaller one 0.  A row of -inf gives 0, +inf and NaN give NaN.
+struct Power { float slope, shift; };
+__device__ __forceinline__ Power power_of(float m, float c) {
+  const float shift = -m * c;
+  if (fabsf(shift) < 1e30f) return Power{c, shift};
+  const uint32_t e = (__float_as_uint(m) >> 23) & 255;   // m is normal, infinite or NaN
+  if (e == 255) return Power{1.f, m == -INFINITY ? 0.f : -m};
+  const float slope = __uint_as_float((127 + 40 + 127 - e) << 23);   // slope m in 2^40 .. 2^41
+  return Power{slope, -m * slope};
 }
 // log-sum-exp of a row's values over the temperature, from their largest one and the sum beside it
 __device__ __forceinline__ float row_lse(const Online& o, float tau) {
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? 7 : 4) void topk_logits_kernel(cons
       top[u] = cm;
       if (who[u] && __any(cm > m)) raise(wave_max(fmaxf(cm, m)));
       float part = 0.f;
-      if (wide) {
+      if (wide) {   // (as power_of, which takes registers that are not there)
 #pragma unroll
         for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f((v[j] - m) * c);
       } else {
@@ -394,62 +397,79 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
 // ----------------------------------------------------------------------------------------------
 namespace {
 
-// A row's teacher, in LDS: entry j's column (-1: none), probability and student logit.
+// A row's teacher, in LDS: entry j's column (-1: none), probability and student logit, the probability of all entries on that
+// column, and (from teacher_finish on) the gradient there.
 struct Teacher {
-  int id[kMaxTeacher];
-  float p[kMaxTeacher], z[kMaxTeacher];
+  alignas(16) int id[kMaxTeacher];
+  float p[kMaxTeacher], z[kMaxTeacher], at[kMaxTeacher], grad[kMaxTeacher];
   float mass, loss;     // P, and sum_j p_j log p_j
   int any;              // whether an entry says anything
 };
 
-// By one wave: everything of the row's teacher that the student's statistics do not enter.  The student's logits at its
-// columns are read here, before anything of the row can be overwritten.
-template <typename T>
-__device__ __forceinline__ void teacher_load(Teacher& te, const T* zr, int V, int k, const int32_t* ids, const float* t, const float* lse, size_t row,
-                                             float tau, int lane) {
-  constexpr int PER = kMaxTeacher / 64;
-  int id[PER];
-  float a[PER], m = -INFINITY;
+// One wave's part of it, in three steps: the entries are requested, then the student's logits at their columns (before anything
+// of the row can be overwritten), and then everything is computed that the student's statistics do not enter.
+constexpr int kTeacherPer = kMaxTeacher / 64;
+struct TeacherRegs { int id[kTeacherPer]; float t[kTeacherPer], z[kTeacherPer], lse; };
+__device__ __forceinline__ void teacher_fetch(TeacherRegs& r, const DistillArgs& a, size_t row, int lane) {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
+  for (int i = 0; i < kTeacherPer; ++i) {
     const int j = lane + 64 * i;
-    id[i] = j < k ? ids[row * (size_t)k + j] : -1;
-    if (id[i] >= V) id[i] = -1;
-    a[i] = id[i] >= 0 ? t[row * (size_t)k + j] / tau : -INFINITY;
-    if (id[i] < 0) id[i] = -1;
+    r.id[i] = j < a.k ? a.ids[row * (size_t)a.k + j] : -1;
+    r.t[i] = j < a.k ? a.t[row * (size_t)a.k + j] : 0.f;
+  }
+  r.lse = a.tlse ? a.tlse[row] : 0.f;
+}
+template <typename T>
+__device__ __forceinline__ void teacher_logits(TeacherRegs& r, const T* zr, int V) {
+#pragma unroll
+  for (int i = 0; i < kTeacherPer; ++i) {
+    if (r.id[i] < 0 || r.id[i] >= V) r.id[i] = -1;
+    r.z[i] = r.id[i] >= 0 ? ldf(zr, (size_t)r.id[i]) : 0.f;
+  }
+}
+__device__ __forceinline__ void teacher_load(Teacher& te, const TeacherRegs& r, const DistillArgs& args, int lane) {
+  float a[kTeacherPer], m = -INFINITY;
+  bool says = false;
+#pragma unroll
+  for (int i = 0; i < kTeacherPer; ++i) {
+    a[i] = r.id[i] >= 0 ? r.t[i] / args.tau : -INFINITY;
+    says |= !(a[i] == -INFINITY);
     m = fmaxf(m, a[i]);
   }
-  bool any = false, nan = false;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    any |= a[i] > -INFINITY;
-    nan |= a[i] != a[i];
-  }
-  any = __any(any || nan);
-  m = wave_max(m);
-  float L;
-  if (lse) {
-    L = lse[row];
-  } else {
+  const bool any = __any(says);
+  float L = r.lse;
+  if (!args.tlse) {
+    m = wave_max(m);
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) s += id[i] >= 0 && any ? expf(a[i] - m) : 0.f;
+    for (int i = 0; i < kTeacherPer; ++i) s += r.id[i] >= 0 && any ? expf(a[i] - m) : 0.f;
     L = m + logf(wave_sum(s));
   }
   float mass = 0.f, ent = 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
+  for (int i = 0; i < kTeacherPer; ++i) {
     const int j = lane + 64 * i;
-    const float p = id[i] >= 0 && any ? expf(a[i] - L) : 0.f;
+    const float p = r.id[i] >= 0 && any ? expf(a[i] - L) : 0.f;
     mass += p;
     ent += p != 0.f ? p * (a[i] - L) : 0.f;
-    te.id[j] = id[i];
+    te.id[j] = r.id[i];
     te.p[j] = p;
-    te.z[j] = id[i] >= 0 ? ldf(zr, (size_t)id[i]) : 0.f;
+    te.z[j] = r.z[i];
   }
   mass = wave_sum(mass);
   ent = wave_sum(ent);
   if (lane == 0) { te.mass = mass; te.loss = ent; te.any = any ? 1 : 0; }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  float at[kTeacherPer] = {};
+#pragma unroll 2
+  for (int j = 0; j < args.k; ++j) {
+    const int id = te.id[j];
+    const float p = te.p[j];
+#pragma unroll
+    for (int i = 0; i < kTeacherPer; ++i) at[i] += id == r.id[i] ? p : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kTeacherPer; ++i) te.at[lane + 64 * i] = at[i];
 }
 // by one wave: sum_j p_j (log p_j - log q_j), with log q_j = (z_j - M) / tau - log S
 __device__ __forceinline__ float teacher_loss(const Teacher& te, int k, const Online& o, float tau, int lane) {
@@ -462,17 +482,93 @@ __device__ __forceinline__ float teacher_loss(const Teacher& te, int k, const On
   }
   return te.loss - wave_sum(x);
 }
-// gradient at a teacher's column: all of the row's probability on it
-__device__ __forceinline__ float teacher_grad(const Teacher& te, int k, int j, float q_mass, float tau) {
-  float p = 0.f;
-  for (int i = 0; i < k; ++i) p += te.id[i] == te.id[j] ? te.p[i] : 0.f;
-  return tau * (q_mass - p);
+
+// What a block knows of its row after the statistics, and what remains but for the dense part of the gradient: the loss, and the
+// gradient at the teacher's columns, all of the row's probability on a column in each of its entries.  One barrier.
+struct RowGrad { bool keep; float scale; };   // dz = scale 2^(c (z - max)) off the teacher's columns
+__device__ __forceinline__ RowGrad teacher_finish(Teacher& te, const DistillArgs& a, size_t row, bool masked, const Online& o, float c, bool grad) {
+  const bool keep = !masked && te.any;
+  const float f = te.mass / o.s;
+  if (threadIdx.x < 64) {
+    const float loss = keep ? a.tau * a.tau * teacher_loss(te, a.k, o, a.tau, threadIdx.x) : 0.f;
+    if (threadIdx.x == 0) { a.lse[row] = row_lse(o, a.tau); a.loss_rows[row] = loss; }
+  }
+  if (grad) {
+    const int j = (int)threadIdx.x - 64;   // (the second wave on)
+    if (j >= 0 && j < a.k) te.grad[j] = a.tau * (f * __builtin_amdgcn_exp2f((te.z[j] - o.m) * c) - te.at[j]);
+    __syncthreads();
+  }
+  return RowGrad{keep, a.tau * f};
+}
+// the teacher's columns, each by the thread that has stored its chunk of E before (a thread's stores to one address stay in order)
+template <typename T, int NT, int E>
+__device__ __forceinline__ void teacher_store(const Teacher& te, int k, T* dr) {
+#pragma unroll 1
+  for (int j = 0; j < k; j += 4) {
+    const int4 id = *reinterpret_cast<const int4*>(&te.id[j]);   // (entries from k on are -1)
+    if (id.x >= 0 && (id.x / E) % NT == (int)threadIdx.x) stf(dr, (size_t)id.x, te.grad[j]);
+    if (id.y >= 0 && (id.y / E) % NT == (int)threadIdx.x) stf(dr, (size_t)id.y, te.grad[j + 1]);
+    if (id.z >= 0 && (id.z / E) % NT == (int)threadIdx.x) stf(dr, (size_t)id.z, te.grad[j + 2]);
+    if (id.w >= 0 && (id.w / E) % NT == (int)threadIdx.x) stf(dr, (size_t)id.w, te.grad[j + 3]);
+  }
+}
+
+__device__ __forceinline__ void store_once8(bf16_t* p, const float (&v)[8]) {
+  typedef unsigned u32x4_nt __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4_nt{f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7])}, reinterpret_cast<u32x4_nt*>(p));
+}
+__device__ __forceinline__ void store_once8(float* p, const float (&v)[8]) {
+  typedef float f32x4_nt __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(f32x4_nt{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_nt*>(p));
+  __builtin_nontemporal_store(f32x4_nt{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4_nt*>(p) + 1);
+}
+
+// A row read from memory, four chunks requested at a time, once for the statistics and once for the gradient.
+template <typename T, int NT>
+__device__ __forceinline__ Online row_stats(const T* zr, int V, float c) {   // of the thread
+  constexpr int U = sizeof(T) == 2 ? 4 : 2, STEP = NT * 8;
+  const int last = (V - 1) / 8 * 8;
+  Online o{-INFINITY, 0.f};
+  for (int base = 0; base < V; base += U * STEP) {
+    Raw8<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u].load(zr, (size_t)min(base + u * STEP + (int)threadIdx.x * 8, last));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = base + u * STEP + threadIdx.x * 8;
+      float v[8];
+      raw[u].get(v);
+      if (base + U * STEP > V) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = col + j < V ? v[j] : -INFINITY;
+      }
+      online_add8(o, v, c);
+    }
+  }
+  return o;
+}
+template <typename T, int NT>
+__device__ __forceinline__ void row_grad(const T* zr, T* dr, int V, int64_t ldz, const RowGrad& g, float m, float c) {
+  constexpr int U = sizeof(T) == 2 ? 4 : 2, STEP = NT * 8;
+  const int last = (int)ldz - 8;
+  for (int base = 0; base < ldz; base += U * STEP) {
+    Raw8<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u].load(zr, (size_t)min(base + u * STEP + (int)threadIdx.x * 8, last));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = base + u * STEP + threadIdx.x * 8;
+      float v[8];
+      raw[u].get(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = g.keep && col + j < V ? g.scale * __builtin_amdgcn_exp2f((v[j] - m) * c) : 0.f;
+      if (col < ldz) store_once8(dr + col, v);
+    }
+  }
 }
 
 }  // namespace
 
-// A block owns a row and reads it twice, for the statistics and for the gradient.  The columns of the teacher's entries are
-// written over by the thread that wrote their eight columns before.
 template <typename T, bool GRAD>
 __global__ __launch_bounds__(512) void distill_kernel(DistillArgs a) {
   constexpr int NT = 512;
@@ -481,52 +577,204 @@ __global__ __launch_bounds__(512) void distill_kernel(DistillArgs a) {
   const size_t row = blockIdx.x;
   const T* zr = (const T*)a.z + row * (size_t)a.ldz;
   const float c = kLog2e / a.tau;
-  const int V = a.V, lane = threadIdx.x & 63;
-  if (threadIdx.x < 64) teacher_load(te, zr, V, a.k, a.ids, a.t, a.tlse, row, a.tau, lane);
-  Online o{-INFINITY, 0.f};
-  for (int i = threadIdx.x * 8; i < V; i += NT * 8) {
-    float v[8];
-    load_tail8(zr, i, V, v);
-    online_add8(o, v, c);
-  }
-  o = online_block<NT>(o, c, sm);
-  const bool keep = a.mask[row] != 0 && te.any;
+  const bool masked = a.mask[row] == 0;
+  TeacherRegs regs;
   if (threadIdx.x < 64) {
-    const float loss = keep ? a.tau * a.tau * teacher_loss(te, a.k, o, a.tau, lane) : 0.f;
-    if (lane == 0) { a.lse[row] = row_lse(o, a.tau); a.loss_rows[row] = loss; }
+    teacher_fetch(regs, a, row, threadIdx.x);
+    teacher_logits(regs, zr, a.V);
   }
+  Online o = row_stats<T, NT>(zr, a.V, c);
+  if (threadIdx.x < 64) teacher_load(te, regs, a, threadIdx.x);
+  o = online_block<NT>(o, c, sm);
+  const RowGrad g = teacher_finish(te, a, row, masked, o, c, GRAD);
   if constexpr (GRAD) {
     T* dr = (T*)a.dz + row * (size_t)a.ldz;
-    const float f = te.mass / o.s;
-    for (int i = threadIdx.x * 8; i < a.ldz; i += NT * 8) {
-      float v[8];
-      if (keep) {
-        load_tail8(zr, i, V, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = i + j < V ? a.tau * f * __builtin_amdgcn_exp2f((v[j] - o.m) * c) : 0.f;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.f;
-      }
-      st8(dr, i, v);
-    }
-    if (keep)
-      for (int j = 0; j < a.k; ++j)
-        if (te.id[j] >= 0 && (te.id[j] >> 3) % NT == (int)threadIdx.x)
-          stf(dr, (size_t)te.id[j], teacher_grad(te, a.k, j, f * __builtin_amdgcn_exp2f((te.z[j] - o.m) * c), a.tau));
+    row_grad<T, NT>(zr, dr, a.V, a.ldz, g, o.m, c);
+    if (g.keep) teacher_store<T, NT, 8>(te, a.k, dr);
   }
 }
+
+// The training call with the row held on its CU between the statistics and the gradient: read once, written once.  A thread
+// keeps the 16-byte chunks t, t + 512, ... of its block's row: the first NREG in registers, all of them wholly below V, the n_lds
+// others in LDS, where padded columns are turned into -inf.  Two passes of exponentials, each one fused step and 2^x per
+// element; 128256 columns of bf16 are 24 chunks in registers and 8 in LDS, 66 KB
+// with the teacher's entries, so that two rows share a CU and the arithmetic of one hides behind the memory traffic of the other.
+// Bound by memory: [8192, 128256] bf16, k = 32: 750 us, 5.6 TB/s (k = 128: 795; read twice: 1210).
+template <typename T, int NREG>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) void distill_resident_kernel(DistillArgs a, int n_lds) {
+  constexpr int NT = 512, E = 16 / (int)sizeof(T), STEP = NT * E;
+  typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+  extern __shared__ u32x4_t distill_row_lds[];                 // n_lds x NT chunks
+  __shared__ Teacher te;
+  __shared__ float red[17];
+  const size_t row = blockIdx.x;
+  const T* zr = (const T*)a.z + row * (size_t)a.ldz;
+  T* dr = (T*)a.dz + row * (size_t)a.ldz;
+  const float c = kLog2e / a.tau;
+  const int V = a.V, c0 = threadIdx.x * E;
+  u32x4_t* mine = distill_row_lds + threadIdx.x;
+  const int bytes = (int)((uint32_t)a.ldz * (uint32_t)sizeof(T));
+  const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(zr), 0, bytes, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rd = __builtin_amdgcn_make_buffer_rsrc(dr, 0, bytes, 0x00020000);
+  auto fetch = [&](int col, int soff) { return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rz, (uint32_t)col * sizeof(T), soff, 2)); };
+  auto store = [&](u32x4_t v, int col, int soff) { __builtin_amdgcn_raw_buffer_store_b128(v, rd, (uint32_t)col * sizeof(T), soff, 2); };
+  const bool masked = a.mask[row] == 0;
+  // Where the row's chunks leave no registers, the teacher's entries are done with before they are requested; else they are requested
+  // before and worked on while the chunks arrive.
+  constexpr bool EARLY = NREG >= 24;
+  TeacherRegs regs;
+  if (threadIdx.x < 64) {
+    teacher_fetch(regs, a, row, threadIdx.x);
+    if constexpr (EARLY) {
+      teacher_logits(regs, zr, V);
+      teacher_load(te, regs, a, threadIdx.x);
+    }
+  }
+  u32x4_t buf[NREG > 0 ? NREG : 1];
+#pragma unroll
+  for (int i = 0; i < NREG; ++i) buf[i] = fetch(c0, i * STEP * (int)sizeof(T));
+  if constexpr (!EARLY)
+    if (threadIdx.x < 64) teacher_logits(regs, zr, V);
+  for (int i = 0; i < n_lds; ++i) {
+    const int col = c0 + (NREG + i) * STEP, nv = V - col;
+    u32x4_t v = fetch(col, 0);
+    if (nv < E) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 2) v[k] = 2 * k + 1 < nv ? v[k] : 2 * k < nv ? ((v[k] & 0xFFFFu) | 0xFF800000u) : 0xFF80FF80u;
+        else v[k] = k < nv ? v[k] : 0xFF800000u;
+      }
+    }
+    mine[i * NT] = v;
+  }
+  if constexpr (!EARLY)
+    if (threadIdx.x < 64) teacher_load(te, regs, a, threadIdx.x);
+
+  // each pass takes the register chunks strictly one after the other, so that no pass keeps their unpacked values
+  auto turn = [&](int i, float& running) { asm volatile("" : "+v"(running), "+v"(buf[i])); };
+  auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+  auto hi = [](uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); };
+  auto max3 = [](float x, float y, float z) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+  };
+  auto chunk_max = [&](u32x4_t v, float m) {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = max3(m, lo(v[k]), hi(v[k]));
+    } else {
+      m = max3(m, __uint_as_float(v[0]), __uint_as_float(v[1]));
+      m = max3(m, __uint_as_float(v[2]), __uint_as_float(v[3]));
+    }
+    return m;
+  };
+  auto power = [&](float x, float slope, float sh) { return __builtin_amdgcn_exp2f(fmaf(x, slope, sh)); };
+  auto chunk_sum = [&](u32x4_t v, float slope, float sh) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 2) s += power(lo(v[k]), slope, sh) + power(hi(v[k]), slope, sh);
+      else s += power(__uint_as_float(v[k]), slope, sh);
+    }
+    return s;
+  };
+  auto chunk_grad = [&](u32x4_t v, float slope, float sh, float f) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 2) v[k] = f2bf2(f * power(lo(v[k]), slope, sh), f * power(hi(v[k]), slope, sh));
+      else v[k] = __float_as_uint(f * power(__uint_as_float(v[k]), slope, sh));
+    }
+    return v;
+  };
+
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NREG; ++i) {
+    turn(i, m);
+    m = chunk_max(buf[i], m);
+  }
+  for (int i = 0; i < n_lds; ++i) m = chunk_max(mine[i * NT], m);
+  m = wave_max(m);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = red[0];
+  for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, red[i]);
+  const Power pw = power_of(m, c);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NREG; ++i) {
+    turn(i, s);
+    s += chunk_sum(buf[i], pw.slope, pw.shift);
+  }
+  for (int i = 0; i < n_lds; ++i) s += chunk_sum(mine[i * NT], pw.slope, pw.shift);
+  const Online o{m, block_sum(s, red)};
+  const RowGrad g = teacher_finish(te, a, row, masked, o, c, true);
+  if (!g.keep) {
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < NREG; ++i) store(zero, c0, i * STEP * (int)sizeof(T));
+    for (int i = 0; i < n_lds; ++i) store(zero, c0 + (NREG + i) * STEP, 0);
+    return;
+  }
+  float sh = pw.shift;
+#pragma unroll
+  for (int i = 0; i < NREG; ++i) {
+    turn(i, sh);
+    buf[i] = chunk_grad(buf[i], pw.slope, sh, g.scale);
+    store(buf[i], c0, i * STEP * (int)sizeof(T));
+  }
+  for (int i = 0; i < n_lds; ++i) store(chunk_grad(mine[i * NT], pw.slope, sh, g.scale), c0 + (NREG + i) * STEP, 0);
+  teacher_store<T, NT, E>(te, a.k, dr);
+}
+
+namespace {
+constexpr int kDistillMaxLds = 17;   // chunks of a thread in LDS: 8 KB of the block's row each, beside the teacher's entries
+// The resident kernel for rows that fit a CU; false where they do not.
+template <typename T>
+bool launch_distill_resident(const DistillArgs& a, hipStream_t s, hipError_t& e) {
+  constexpr int STEP = 512 * 16 / (int)sizeof(T);
+  const int64_t chunks = (a.ldz + STEP - 1) / STEP, whole = a.V / STEP;
+  static const int kRegs[] = {24, 20, 16, 12, 8, 7, 6, 4, 2, 1, 0};
+  int nreg = 0;
+  for (int r : kRegs)
+    if (r <= whole) { nreg = r; break; }
+  const int64_t n_lds = chunks - nreg;
+  if (n_lds > kDistillMaxLds) return false;
+  const size_t lds = (size_t)n_lds * 512 * 16;
+  const void* kernel = nullptr;
+#define TIDE_DISTILL(R) case R: kernel = (const void*)distill_resident_kernel<T, R>; break
+  switch (nreg) {
+    TIDE_DISTILL(24); TIDE_DISTILL(20); TIDE_DISTILL(16); TIDE_DISTILL(12); TIDE_DISTILL(8);
+    TIDE_DISTILL(7); TIDE_DISTILL(6); TIDE_DISTILL(4); TIDE_DISTILL(2); TIDE_DISTILL(1); TIDE_DISTILL(0);
+  }
+#undef TIDE_DISTILL
+  e = hipSuccess;
+  if (lds > 65536 - 4096) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kDistillMaxLds * 512 * 16);
+  if (e != hipSuccess) return true;
+  DistillArgs args = a;
+  int n = (int)n_lds;
+  void* params[] = {&args, &n};
+  e = hipLaunchKernel(kernel, dim3((unsigned)a.rows), dim3(512), params, lds, s);
+  return true;
+}
+}  // namespace
 
 hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s) {
   if (a.rows <= 0) return hipSuccess;
   const bool grad = a.dz != nullptr;
   ProfScope ps(grad ? "distill_train" : "distill_eval", 0, (double)a.rows * dtype_size(dtype) * (a.V + (grad ? (double)a.ldz : 0.0)), s);
+  hipError_t e;
+  if (grad && (dtype == kBF16 ? launch_distill_resident<bf16_t>(a, s, e) : launch_distill_resident<float>(a, s, e))) return e;
   const dim3 grid((unsigned)a.rows), blk(512);
+  // LDS that goes unused holds the gradient's rows in flight to two per CU, so that the second read finds them in the last cache: us with / without,
+  // fp32 [4096, 128256] 1070 / 1277, [4096, 100001] 804 / 935.
+  const size_t pad = 52 * 1024;
   if (dtype == kBF16) {
-    if (grad) hipLaunchKernelGGL((distill_kernel<bf16_t, true>), grid, blk, 0, s, a);
+    if (grad) hipLaunchKernelGGL((distill_kernel<bf16_t, true>), grid, blk, pad, s, a);
     else hipLaunchKernelGGL((distill_kernel<bf16_t, false>), grid, blk, 0, s, a);
   } else {
-    if (grad) hipLaunchKernelGGL((distill_kernel<float, true>), grid, blk, 0, s, a);
+    if (grad) hipLaunchKernelGGL((distill_kernel<float, true>), grid, blk, pad, s, a);
     else hipLaunchKernelGGL((distill_kernel<float, false>), grid, blk, 0, s, a);
   }
   return hipGetLastError();
