@@ -196,7 +196,7 @@ __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int la
 
 // (256 threads in 89 registers, five blocks on a CU: 365 us where seven take 327)
 template <typename T, int NT, int U, int D>
-__global__ __launch_bounds__(NT, NT == 256 ? 7 : 4) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
+__global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_logits_kernel(const T* __restrict__ z, int64_t ldz, int V, int k, float tau,
                                                          int32_t* __restrict__ ids, float* __restrict__ values,
                                                          float* __restrict__ lse) {
   constexpr int NW = NT / 64, ROUND = NT * U * 8;
@@ -375,6 +375,7 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
   // Up to a row per CU, all of a CU's threads on it, and four rounds requested at a time; two rows, half of them; beyond, four waves a row
   // (us, 1024 / 512 / 256 threads, [rows, 128256] bf16, k = 32: 61 rows 27 / 29 / 43, 256 30 / 32 / 44, 512 57 / 39 / 49,
   // 1024 108 / 72 / 59).
+  // (Eight blocks a CU in fp32, without a round requested ahead, against seven with one: [1999, 32001] 57 / 61 us; bf16 [8192, 128256] 334 / 326.)
   const int nt = rows <= 256 ? 1024 : rows <= 512 ? 512 : 256;
 #define TIDE_TOPK(T, NT, U, D) hipLaunchKernelGGL((topk_logits_kernel<T, NT, U, D>), grid, dim3(NT), 0, s, (const T*)z, ldz, V, k, tau, ids, values, lse)
   if (dtype == kBF16) {
@@ -384,7 +385,7 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
   } else {
     if (nt == 1024) TIDE_TOPK(float, 1024, 2, 4);
     else if (nt == 512) TIDE_TOPK(float, 512, 2, 2);
-    else TIDE_TOPK(float, 256, 2, 2);
+    else TIDE_TOPK(float, 256, 2, 1);
   }
 #undef TIDE_TOPK
   return hipGetLastError();

@@ -71,6 +71,9 @@ struct MfmaParams {
   float* split_scratch;
 };
 struct MfmaAdamParams : MfmaParams { AdamTarget adam; };
+// The LM head's logits (NT) that are not kept: their statistics, or their gradient, in place of the product (see lm_stats, lm_grad below).
+struct MfmaLmParams : MfmaParams { LmTarget lm; };
+enum : int { kLmNone = 0, kLmStats = 1, kLmGrad = 2 };
 enum : int { kSplitNone = 0, kSplitTail = 1, kSplitAll = 2 };
 
 // How a launch whose tiles do not fill the chip is split over K.  ns, measured on 256 x 256 and on 128 x 128 tiles:
@@ -320,8 +323,8 @@ __device__ __forceinline__ void adam_store(const AdamTarget& t, const AdamRate& 
 // ------------------------------------------------------------------------------------------------
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-template <int BM, int BN, bool AMM, bool BNM, typename TO, bool KWHOLE, bool ADAM, bool LONG = false>
-__device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamParams, MfmaParams> p, int pid) {   // pid: which of the launch's blocks
+template <int BM, int BN, bool AMM, bool BNM, typename TO, bool KWHOLE, bool ADAM, bool LONG = false, int LM = kLmNone>
+__device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamParams, std::conditional_t<LM != kLmNone, MfmaLmParams, MfmaParams>> p, int pid) {   // pid: which of the launch's blocks
   static_assert(BN == 256 ? BM % 32 == 0 && BM >= 128 && BM <= 256 : BN == 128 && BM == 128, "tile edges");
   constexpr int BK = 64, WAVES_M = 2, WAVES_N = BN / 64, NW = WAVES_M * WAVES_N;
   constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N;   // BM / 2 x 64
@@ -620,6 +623,122 @@ __device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamPara
     }
   };
 
+  // ---- epilogues of logits that are not kept.  z = the accumulators; token(row) - first column of the wave = the label's place in it. ----
+  // Forward: of every row, the maximum and the sum of exponentials over this tile's columns (a row of a wave's 64 columns lies in four
+  // lanes of 16 values; the waves side by side meet in LDS), and the label's logit from the one tile that holds it.
+  // 256 x 256: 128 exponentials a lane, about 4 us behind 85 us of products at K = 4096.
+  [[maybe_unused]] auto lm_stats = [&](bf16_t* lds) {
+    if constexpr (LM == kLmStats) {
+      constexpr float LOG2E = 1.4426950408889634f;
+      float2* st = reinterpret_cast<float2*>(lds);   // [WAVES_N][BM]
+      const int wm0 = m0 + wave_m * WM, wn0 = n0 + wave_n * WN;
+      int label[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) label[i] = p.lm.tokens[max(0, min(wm0 + 16 * i + lc, p.M - 1))] - wn0;
+      const bool ragged = n0 + BN > p.N;
+      __builtin_amdgcn_s_barrier();                  // the other waves' operand reads
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int gm = wm0 + 16 * i + lc;
+        if (ragged) {
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (wn0 + 16 * j + 4 * lg + q >= p.N) acc[i][j][q] = -INFINITY;
+        }
+        const bool mine = gm < p.M && label[i] >= 0 && label[i] < WN && ((label[i] >> 2) & 3) == lg;
+        if (__any(mine)) {
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (mine && label[i] == 16 * j + 4 * lg + q) p.lm.label[gm] = acc[i][j][q];
+        }
+        float m = acc[i][0][0];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) m = fmaxf(m, acc[i][j][q]);
+        m = fmaxf(m, __shfl_xor(m, 16, 64));
+        m = fmaxf(m, __shfl_xor(m, 32, 64));
+        const float shift = m == -INFINITY ? 0.f : -m * LOG2E;
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], LOG2E, shift));
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        if (lg == 0) st[wave_n * BM + wave_m * WM + 16 * i + lc] = make_float2(m, s);
+      }
+      __syncthreads();
+      for (int r = tid; r < BM; r += NW * 64) {
+        float2 o = st[r];
+#pragma unroll
+        for (int w = 1; w < WAVES_N; ++w) {
+          const float2 x = st[w * BM + r];
+          const float m = fmaxf(o.x, x.x);
+          if (m > -INFINITY) o.y = o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E) + x.y * __builtin_amdgcn_exp2f((x.x - m) * LOG2E);
+          o.x = m;
+        }
+        if (m0 + r < p.M) p.lm.part[(size_t)tile_n * p.lm.part_ld + m0 + r] = o;
+      }
+    }
+  };
+  // Backward: dz = weight (exp(z - lse) - [label]) in bf16, through the wave's LDS patch in row segments of 16 bytes like any bf16 result.
+  [[maybe_unused]] auto lm_grad = [&](bf16_t* patch) {
+    if constexpr (LM == kLmGrad) {
+      constexpr float LOG2E = 1.4426950408889634f;
+      constexpr int PIECES = WN / 8, PP = WN + 8;
+      const int wm0 = m0 + wave_m * WM, wn0 = n0 + wave_n * WN;
+      bf16_t* C = reinterpret_cast<bf16_t*>(p.C);
+      LmRow row[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) row[i] = p.lm.rows[max(0, min(wm0 + 16 * i + lc, p.M - 1))];
+      __builtin_amdgcn_s_barrier();
+#pragma unroll
+      for (int i2 = 0; i2 < TM2; ++i2) {
+#pragma unroll
+        for (int ih = 0; ih < min(2, TM - 2 * i2); ++ih) {
+          const int i = 2 * i2 + ih;
+          const int label = row[i].token - p.lm.n0 - wn0;
+          const bool mine = label >= 0 && label < WN && ((label >> 2) & 3) == lg;
+          f32x4_t v[TN];
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[j][q] = row[i].weight * __builtin_amdgcn_exp2f(fmaf(acc[i][j][q], LOG2E, row[i].shift));
+          if (__any(mine)) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (mine && label == 16 * j + 4 * lg + q) v[j][q] -= row[i].weight;
+          }
+          if (wn0 < p.lm.zero) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (wn0 + 16 * j + 4 * lg + q < p.lm.zero) v[j][q] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+            *reinterpret_cast<uint2*>(patch + (16 * ih + lc) * PP + 16 * j + 4 * lg) = make_uint2(f2bf2(v[j][0], v[j][1]), f2bf2(v[j][2], v[j][3]));
+        }
+#pragma unroll
+        for (int t = 0; t < 16 * min(2, TM - 2 * i2) * PIECES / 64; ++t) {
+          const int pc = lane + 64 * t;
+          const int r = pc / PIECES, piece = pc % PIECES;
+          const int gm = wm0 + 32 * i2 + r, gn = wn0 + piece * 8;
+          const u32x4_t val = *reinterpret_cast<const u32x4_t*>(patch + r * PP + piece * 8);
+          if (gm < p.M && gn < p.N) *reinterpret_cast<u32x4_t*>(C + (size_t)gm * p.ldc + gn) = val;
+        }
+      }
+    }
+  };
+
   u32x4_t fa0[GA], fa1[GA], fb0[TN], fb1[TN];
   {
     // ---- slabs of 64: THREE LDS units for one operand and TWO for the other (5 x 32 KiB = all of the 160 KiB) ----
@@ -905,11 +1024,17 @@ __device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamPara
     }
     }
     TIDE_WAIT_VMCNT(0);   // dummy slabs still in flight write LDS: let them land before the patches are written
+    if constexpr (LM == kLmStats) {
+      static_assert(WAVES_N * BM * 8 <= D_STAGE * 2, "the rows' statistics fit a unit");
+      lm_stats(ld0);
+      return;
+    }
     constexpr int PPU = D_STAGE / kPatchElems;   // epilogue patches per deep unit; a wave left over takes the first shallow one
     static_assert(PPU >= 1 && S_STAGE >= kPatchElems && NW <= 3 * PPU + 1, "the epilogue patches fit four units");
     const int pu = wave / PPU;
     bf16_t* unit = pu == 0 ? ld0 : (pu == 1 ? ld1 : (pu == 2 ? ld2 : ls0));
-    epilogue(unit + (wave % PPU) * kPatchElems);
+    if constexpr (LM == kLmGrad) lm_grad(unit + (wave % PPU) * kPatchElems);
+    else epilogue(unit + (wave % PPU) * kPatchElems);
   }
 }
 
@@ -921,6 +1046,11 @@ __global__ __launch_bounds__(2 * BN) void gemm_mfma_kernel(std::conditional_t<AD
 template <bool AMM, bool BNM, typename TO, bool KWHOLE>
 __global__ __launch_bounds__(256) void gemm_mfma_few_kernel(MfmaParams p) {
   gemm_block<128, 128, AMM, BNM, TO, KWHOLE, false, true>(p, blockIdx.x);
+}
+
+template <int BM, int BN, bool KWHOLE, int LM>
+__global__ __launch_bounds__(2 * BN) void gemm_mfma_lm_kernel(MfmaLmParams p) {
+  gemm_block<BM, BN, false, false, bf16_t, KWHOLE, false, false, LM>(p, blockIdx.x);
 }
 
 // The weight gradients of a layer with their updates, product after product over the blocks of one launch.  A product of few rows is
@@ -1475,6 +1605,57 @@ hipError_t launch_gemm_adam(const GemmArgs& a, const AdamTarget& t, hipStream_t 
   const hipError_t e = launch_layout<true, true, float>(p, lp, s);
   return e != hipSuccess || p.split != kSplitTail ? e : launch_fixup<true>(p, t, s);
 }
+
+namespace {
+template <int BM, int BN, int LM>
+hipError_t launch_lm_tiles(MfmaLmParams& p, hipStream_t s) {
+  p.tiles_m = (p.M + BM - 1) / BM;
+  p.tiles_n = (p.N + BN - 1) / BN;
+  const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(2 * BN);
+  if constexpr (BM == BN) {
+    if (!whole_slabs(p)) {
+      hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, BN, false, LM>), grid, blk, 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, BN, true, LM>), grid, blk, 0, s, p);
+  return hipGetLastError();
+}
+// Tiles of the head's logits: the cheapest by the costs that all products are planned with, of whole tiles only (and with a ragged K of
+// the squares); of the heights, those that the others come close to.
+LaunchPlan plan_lm(const GemmArgs& a) {
+  LaunchPlan best{128, 128, kSplitNone, {1, 0, 0}, {0, 0, 0}};
+  int64_t least = -1;
+  for (const int BM : {128, 192, 256, 0}) {
+    const LaunchPlan lp{BM ? BM : 128, BM ? 256 : 128, kSplitNone, {1, 0, 0}, {0, 0, 0}};
+    if (lp.BM != lp.BN && a.K % 64) continue;
+    if (BM == 0 && tile_count(a.M, a.N, 256) >= 4096) continue;   // (statistics of half as many columns each: callers hold memory for those of 256 then)
+    int64_t t = 0;
+    for (int share = 10; share <= 20; ++share) t += launch_time(a, lp, std::max<int64_t>(1, a.M * share / 20));
+    if (least < 0 || t < least) { least = t; best = lp; }
+  }
+  return best;
+}
+template <int LM>
+hipError_t launch_lm(const GemmArgs& a, const LmTarget& t, hipStream_t s) {
+  if (a.layout != kNT || !gemm_mfma_supported(a) || a.A2 || (LM == kLmGrad && (a.N % 8 || a.ldc % 8 || ((uintptr_t)a.C & 15)))) return hipErrorInvalidValue;
+  const LaunchPlan lp = plan_lm(a);
+  MfmaLmParams p;
+  fill_params(p, a, lp);
+  p.lm = t;
+  ProfScope ps(LM == kLmStats ? "lm_ce_stats" : "lm_ce_grad", 2.0 * (double)a.M * (double)a.N * (double)a.K,
+               2.0 * (double)a.K * ((double)a.M + (double)a.N) + (LM == kLmGrad ? 2.0 * (double)a.M * (double)a.N : 0.0), s);
+  if (a.m_dev) prof_dynamic(a.m_dev, a.m_off, a.M);
+  if (lp.BN == 128) return launch_lm_tiles<128, 128, LM>(p, s);
+  if (lp.BM == 128) return launch_lm_tiles<128, 256, LM>(p, s);
+  if (lp.BM == 192) return launch_lm_tiles<192, 256, LM>(p, s);
+  return launch_lm_tiles<256, 256, LM>(p, s);
+}
+}  // namespace
+
+int gemm_lm_stat_columns(const GemmArgs& a) { return plan_lm(a).BN; }
+hipError_t launch_gemm_lm_stats(const GemmArgs& a, const LmTarget& t, hipStream_t s) { return launch_lm<kLmStats>(a, t, s); }
+hipError_t launch_gemm_lm_grad(const GemmArgs& a, const LmTarget& t, hipStream_t s) { return launch_lm<kLmGrad>(a, t, s); }
 
 namespace {
 template <int BM, int BN>
