@@ -48,8 +48,10 @@ Piece piece_at(const Pieces& p, int i) {   // i = 0: the last one
 // elements between two rows of a piece
 int64_t piece_ld(const Pieces& p) { return (int64_t)align_up((size_t)p.width, 64); }
 
+constexpr int64_t kCountRows = 1024, kDirectRows = 8192;   // see lm_begin_kernel
+
 struct LmCePlan {
-  size_t plan_cnt, scal, cnt, status, kept_idx, row_pos, mask_eff, mask_c, tokens_c, rows_c, y_c;
+  size_t counts, cnt, kept_idx, row_pos, tokens_c, rows_c, y_c;
   size_t z, acc, dy_c, split, split_bytes;   // z: a piece (bf16: of dz), or the forward pass's statistics
   size_t total;
 };
@@ -70,14 +72,10 @@ LmCePlan make_plan(int64_t rows, int64_t V, int64_t d, int dtype) {
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
   const size_t T = (size_t)rows, es = dtype_size(dtype);
   const Pieces pc = plan_pieces(rows, V, dtype);
-  p.plan_cnt = take(plan_rows_scratch_bytes(rows));
-  p.scal = take(64);
+  p.counts = take((T + kCountRows - 1) / kCountRows * 4);
   p.cnt = take(64);
-  p.status = take(64);
   p.kept_idx = take(T * 4);
   p.row_pos = take(T * 4);
-  p.mask_eff = take(T);
-  p.mask_c = take(T);
   p.tokens_c = take(T * 4);
   p.rows_c = take(T * sizeof(LmRow));
   p.y_c = take(T * d * es);
@@ -105,22 +103,98 @@ static_assert(sizeof(RowState) <= sizeof(LmRow), "one array for either");
 
 }  // namespace
 
-// what the products need of every compact row: the log-sum-exp, its weight and its label (backward; fp32's forward: nothing seen yet)
-__global__ __launch_bounds__(256) void lm_rows_kernel(const float* __restrict__ lse, const float* __restrict__ weights, const int32_t* __restrict__ tokens_c,
-                                                      const int32_t* __restrict__ kept_idx, const int* __restrict__ cnt, void* __restrict__ rows, int backward) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= *cnt) return;
-  if (backward) {
-    const int r = kept_idx[i];
-    reinterpret_cast<LmRow*>(rows)[i] = LmRow{-lse[r] * 1.4426950408889634f, weights ? weights[r] : 1.f, tokens_c[i], lse[r]};
-  } else {
-    reinterpret_cast<RowState*>(rows)[i] = RowState{-INFINITY, 0.f, 0.f};
+__device__ __forceinline__ bool kept(const int32_t* tokens, const uint8_t* mask, int64_t t, int V) {
+  const int tk = tokens[t];
+  return mask[t] != 0 && tk >= 0 && tk < V;
+}
+__device__ __forceinline__ int block_count(int n, int* red) {   // of 256 threads; every thread gets the sum
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
+  __syncthreads();
+  return red[0] + red[1] + red[2] + red[3];
+}
+// kept rows of every kCountRows
+__global__ __launch_bounds__(256) void lm_count_kernel(const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, int64_t T, int V,
+                                                       int* __restrict__ counts) {
+  __shared__ int red[4];
+  int n = 0;
+  for (int64_t t = blockIdx.x * kCountRows + threadIdx.x; t < min(T, (blockIdx.x + 1) * kCountRows); t += 256) n += kept(tokens, mask, t, V) ? 1 : 0;
+  n = block_count(n, red);
+  if (threadIdx.x == 0) counts[blockIdx.x] = n;
+}
+
+// The dense array of the kept rows, in order, with everything that a call needs of each: its hidden state, label, place in the batch, and
+// either a fresh RowState (fp32's forward) or its LmRow (backward).  Eight rows per block, two per wave.  The rows kept before a
+// block's are counted by the block itself up to kDirectRows (at most 32 rows per thread), beyond from the counts of
+// kCountRows each: one launch (of 5 us next to nothing in it) instead of three, or two.
+enum : int { kBeginForward = 0, kBeginForwardFp32 = 1, kBeginBackward = 2 };
+struct LmBegin {
+  const void* y; const int32_t* tokens; const uint8_t* mask; const float* weights;
+  float *lse, *loss_rows;
+  void* y_c; int32_t *tokens_c, *kept_idx, *row_pos; int* cnt; void* rows_c;
+  const int* counts;
+  int64_t T;
+  int V, d, mode;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void lm_begin_kernel(LmBegin a) {
+  constexpr int ROWS = 8;
+  __shared__ int red[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t t0 = (int64_t)blockIdx.x * ROWS;
+  int before = 0;
+  int64_t from = 0;
+  if (a.counts) {
+    from = t0 / kCountRows * kCountRows;
+    for (int64_t i = threadIdx.x; i < t0 / kCountRows; i += 256) before += a.counts[i];
+  }
+#pragma unroll 4
+  for (int64_t t = from + threadIdx.x; t < t0; t += 256) before += kept(a.tokens, a.mask, t, a.V) ? 1 : 0;
+  before = block_count(before, red);
+  const bool mine = lane < ROWS && t0 + lane < a.T && kept(a.tokens, a.mask, t0 + lane, a.V);
+  const uint32_t keep = (uint32_t)__ballot(mine);
+  if (t0 + ROWS >= a.T && threadIdx.x == 0) *a.cnt = before + __popc(keep);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = wave * 2 + h;
+    const int64_t t = t0 + r;
+    if (t >= a.T) return;
+    if (!((keep >> r) & 1)) {
+      if (lane == 0) {
+        a.row_pos[t] = -1;
+        if (a.mode != kBeginBackward) a.lse[t] = a.loss_rows[t] = 0.f;
+      }
+      continue;
+    }
+    const int pos = before + __popc(keep & ((1u << r) - 1));
+    if (lane == 0) {
+      const int token = a.tokens[t];
+      a.row_pos[t] = pos;
+      a.kept_idx[pos] = (int32_t)t;
+      a.tokens_c[pos] = token;
+      if (a.mode == kBeginBackward) reinterpret_cast<LmRow*>(a.rows_c)[pos] = LmRow{-a.lse[t] * 1.4426950408889634f, a.weights ? a.weights[t] : 1.f, token, a.lse[t]};
+      else if (a.mode == kBeginForwardFp32) reinterpret_cast<RowState*>(a.rows_c)[pos] = RowState{-INFINITY, 0.f, 0.f};
+    }
+    const T* src = (const T*)a.y + (size_t)t * a.d;
+    T* dst = (T*)a.y_c + (size_t)pos * a.d;
+    if (a.d % 8 == 0) {
+#pragma unroll 4
+      for (int c = lane * 8; c < a.d; c += 64 * 8) {
+        float v[8];
+        ld8(src, c, v);
+        st8(dst, c, v);
+      }
+    } else {
+      for (int c = lane; c < a.d; c += 64) dst[c] = src[c];
+    }
   }
 }
 
-// fp32: one block per row, a piece's columns join the row's statistics
+// fp32: one block per row, a piece's columns join the row's statistics; with the last piece they are complete
 __global__ __launch_bounds__(256) void lm_stats_kernel(const float* __restrict__ z, int64_t ldz, int n0, int n, const int32_t* __restrict__ tokens,
-                                                       const int* __restrict__ cnt, RowState* __restrict__ st) {
+                                                       const int* __restrict__ cnt, RowState* __restrict__ st, int last, const int32_t* __restrict__ kept_idx,
+                                                       float* __restrict__ lse, float* __restrict__ loss_rows) {
   __shared__ float sm[4];
   __shared__ float red[17];
   const int row = blockIdx.x;
@@ -139,38 +213,26 @@ __global__ __launch_bounds__(256) void lm_stats_kernel(const float* __restrict__
   s = block_sum(s, red);
   if (threadIdx.x == 0) {
     const int t = tokens[row] - n0;
-    st[row] = RowState{m, (o.m == -INFINITY ? o.s : o.s * expf(o.m - m)) + s, t >= 0 && t < n ? zr[t] : o.z};
+    const RowState x{m, (o.m == -INFINITY ? o.s : o.s * expf(o.m - m)) + s, t >= 0 && t < n ? zr[t] : o.z};
+    if (last) {
+      const float log_s = logf(x.s);
+      const int at = kept_idx[row];
+      lse[at] = x.m + log_s;
+      loss_rows[at] = log_s + (x.m - x.z);
+    } else {
+      st[row] = x;
+    }
   }
-}
-
-__global__ __launch_bounds__(256) void lm_loss_kernel(int64_t T, const int32_t* __restrict__ row_pos, const RowState* __restrict__ st, float* __restrict__ lse,
-                                                      float* __restrict__ loss_rows) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= T) return;
-  const int i = row_pos[t];
-  if (i < 0) {
-    lse[t] = 0.f;
-    loss_rows[t] = 0.f;
-    return;
-  }
-  const RowState o = st[i];
-  const float log_s = logf(o.s);
-  lse[t] = o.m + log_s;
-  loss_rows[t] = log_s + (o.m - o.z);
 }
 
 // bf16: a row's statistics of all tiles as one.  Sixteen rows per block (their pairs lie side by side), sixteen threads each.
-__global__ __launch_bounds__(256) void lm_join_kernel(int64_t T, const float2* __restrict__ part, int64_t part_ld, int tiles, const float* __restrict__ label,
-                                                      const int32_t* __restrict__ kept_idx, const int32_t* __restrict__ row_pos, const int* __restrict__ cnt,
+__global__ __launch_bounds__(256) void lm_join_kernel(const float2* __restrict__ part, int64_t part_ld, int tiles, const float* __restrict__ label,
+                                                      const int32_t* __restrict__ kept_idx, const int* __restrict__ cnt,
                                                       float* __restrict__ lse, float* __restrict__ loss_rows) {
   __shared__ float2 st[16][17];
   const int r = threadIdx.x & 15, by = threadIdx.x >> 4;
   const int64_t i = (int64_t)blockIdx.x * 16 + r;
   const int n = *cnt;
-  if (by == 0 && i < T && row_pos[i] < 0) {   // (as a row of the batch, not of the compact array)
-    lse[i] = 0.f;
-    loss_rows[i] = 0.f;
-  }
   float2 o = make_float2(-INFINITY, 0.f);
   auto join = [](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x);
@@ -239,14 +301,18 @@ struct LmCe {
   const int* cnt() const { return at<const int>(p.cnt); }
 
   hipError_t begin(bool backward) {
-    LM_TRY(launch_plan_rows(a.tokens, a.mask, a.rows, (int)a.V, 0, at<float>(p.scal), at<int>(p.cnt), at<int32_t>(p.kept_idx), at<int32_t>(p.row_pos),
-                            nullptr, 0, 0, at<uint8_t>(p.mask_eff), at<int>(p.status), at<int>(p.plan_cnt), nullptr, 0, 0, 0.f, nullptr, s));
-    LM_TRY(launch_gather_rows(a.rows, (int)a.d, a.y, ws + p.y_c, 0, nullptr, nullptr, a.tokens, a.mask, at<int32_t>(p.kept_idx), cnt(),
-                              at<int32_t>(p.tokens_c), at<uint8_t>(p.mask_c), a.dtype, s));
-    if (!backward && a.dtype == kBF16) return hipSuccess;
-    ProfScope ps("lm_ce_rows", 0, 32.0 * (double)a.rows, s);
-    hipLaunchKernelGGL(lm_rows_kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, s, a.lse, a.row_weights, at<int32_t>(p.tokens_c),
-                       at<int32_t>(p.kept_idx), cnt(), (void*)(ws + p.rows_c), backward ? 1 : 0);
+    ProfScope ps("lm_ce_begin", 0, 2.0 * (double)a.rows * a.d * dtype_size(a.dtype), s);
+    const bool direct = a.rows <= kDirectRows;
+    if (!direct) {
+      hipLaunchKernelGGL(lm_count_kernel, dim3((unsigned)((a.rows + kCountRows - 1) / kCountRows)), dim3(256), 0, s, a.tokens, a.mask, a.rows, (int)a.V, at<int>(p.counts));
+      LM_TRY(hipGetLastError());
+    }
+    const LmBegin b{a.y, a.tokens, a.mask, a.row_weights, a.lse, a.loss_rows, ws + p.y_c, at<int32_t>(p.tokens_c), at<int32_t>(p.kept_idx),
+                    at<int32_t>(p.row_pos), at<int>(p.cnt), ws + p.rows_c, direct ? nullptr : at<int>(p.counts), a.rows, (int)a.V, (int)a.d,
+                    backward ? kBeginBackward : a.dtype == kF32 ? kBeginForwardFp32 : kBeginForward};
+    const dim3 grid((unsigned)((a.rows + 7) / 8)), blk(256);
+    if (a.dtype == kBF16) hipLaunchKernelGGL(lm_begin_kernel<bf16_t>, grid, blk, 0, s, b);
+    else hipLaunchKernelGGL(lm_begin_kernel<float>, grid, blk, 0, s, b);
     return hipGetLastError();
   }
   const char* piece_w(const Piece& q) const { return (const char*)a.w + (size_t)q.n0 * a.d * dtype_size(a.dtype); }
@@ -275,8 +341,8 @@ hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s) {
     LM_TRY(launch_gemm_lm_stats(g, t, s));
     ProfScope ps("lm_ce_join", 0, 8.0 * (double)a.rows * tiles, s);
     prof_dynamic(c.cnt(), 0, a.rows);
-    hipLaunchKernelGGL(lm_join_kernel, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, a.rows, t.part, t.part_ld, tiles, label,
-                       c.at<int32_t>(c.p.kept_idx), c.at<int32_t>(c.p.row_pos), c.cnt(), a.lse, a.loss_rows);
+    hipLaunchKernelGGL(lm_join_kernel, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, t.part, t.part_ld, tiles, label,
+                       c.at<int32_t>(c.p.kept_idx), c.cnt(), a.lse, a.loss_rows);
     return hipGetLastError();
   }
   for (int i = 0; i < c.pc.count; ++i) {
@@ -285,13 +351,11 @@ hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s) {
     ProfScope ps("lm_ce_stats_fp32", 0, 8.0 * (double)a.rows * q.n, s);
     prof_dynamic(c.cnt(), 0, a.rows);
     hipLaunchKernelGGL(lm_stats_kernel, dim3((unsigned)a.rows), dim3(256), 0, s, c.at<float>(c.p.z), piece_ld(c.pc), (int)q.n0, (int)q.n,
-                       c.at<int32_t>(c.p.tokens_c), c.cnt(), c.at<RowState>(c.p.rows_c));
+                       c.at<int32_t>(c.p.tokens_c), c.cnt(), c.at<RowState>(c.p.rows_c), i + 1 == c.pc.count ? 1 : 0, c.at<int32_t>(c.p.kept_idx),
+                       a.lse, a.loss_rows);
     LM_TRY(hipGetLastError());
   }
-  ProfScope ps("lm_ce_loss", 0, 24.0 * (double)a.rows, s);
-  hipLaunchKernelGGL(lm_loss_kernel, dim3((unsigned)((a.rows + 255) / 256)), dim3(256), 0, s, a.rows, c.at<int32_t>(c.p.row_pos),
-                     c.at<RowState>(c.p.rows_c), a.lse, a.loss_rows);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
