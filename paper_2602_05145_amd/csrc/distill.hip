@@ -2,6 +2,8 @@
 //   topk_logits   the k largest logits of every row, in order, with the row's log-sum-exp
 //   distill       KL divergence of a student's logits from a teacher's top logits, and its gradient
 // Both pass over [rows, vocab] arrays of logits that do not fit any cache: what bounds them is memory.
+#include <type_traits>
+
 #include "kernels.h"
 #include "prof.h"
 #include "tide_common.h"
@@ -26,6 +28,32 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t order_pair(float v, int idx) { return ((uint64_t)order_key(v) << 32) | (uint32_t)~idx; }
 
+// Maximum and sum over a wave on the vector unit alone (a shuffle through LDS takes ten times as long, and a row's few blocks wait for each);
+// every lane gets the result.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float v, float none) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63)); }
+__device__ __forceinline__ float fast_max(float v) {
+  v = fmaxf(v, dpp<0x111, 0xf>(v, -INFINITY));   // from 1, 2, 4 and 8 lanes below in a row of 16
+  v = fmaxf(v, dpp<0x112, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x114, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x118, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x142, 0xa>(v, -INFINITY));   // the row below's last lane, in rows 1 and 3; then the lower half's, in the upper
+  v = fmaxf(v, dpp<0x143, 0xc>(v, -INFINITY));
+  return last_lane(v);
+}
+__device__ __forceinline__ float fast_sum(float v) {
+  v += dpp<0x111, 0xf>(v, 0.f);
+  v += dpp<0x112, 0xf>(v, 0.f);
+  v += dpp<0x114, 0xf>(v, 0.f);
+  v += dpp<0x118, 0xf>(v, 0.f);
+  v += dpp<0x142, 0xa>(v, 0.f);
+  v += dpp<0x143, 0xc>(v, 0.f);
+  return last_lane(v);
+}
+
 // Running (max, sum of 2^(c (z - max))) over eight more values.  The difference comes first: it is 0 for the largest value whatever
 // that is, also where c times it has no number (columns masked with the type's lowest value).
 struct Online { float m, s; };
@@ -41,26 +69,18 @@ __device__ __forceinline__ void online_add8(Online& o, const float (&v)[8], floa
   o.s = (o.m == -INFINITY ? o.s : o.s * __builtin_amdgcn_exp2f((o.m - nm) * c)) + part;   // (before any number: 0, or NaN)
   o.m = nm;
 }
-__device__ __forceinline__ Online online_join(const Online& a, const Online& b, float c) {
-  const float nm = fmaxf(a.m, b.m);
-  const float sa = a.m == -INFINITY ? a.s : a.s * __builtin_amdgcn_exp2f((a.m - nm) * c);   // (a NaN in the sum stays)
-  const float sb = b.m == -INFINITY ? b.s : b.s * __builtin_amdgcn_exp2f((b.m - nm) * c);
-  return Online{nm, sa + sb};
-}
 // of a block of NT threads; every thread gets the result.  sm: NT / 64 pairs.  Two barriers.
 template <int NT>
-__device__ __forceinline__ Online online_block(Online o, float c, Online* sm) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const Online x{__shfl_xor(o.m, d, 64), __shfl_xor(o.s, d, 64)};
-    o = online_join(o, x, c);
-  }
+__device__ __forceinline__ Online online_block(const Online& o, float c, Online* sm) {
+  auto scaled = [&](const Online& x, float m) { return x.m == -INFINITY ? x.s : x.s * __builtin_amdgcn_exp2f((x.m - m) * c); };   // (a NaN in the sum stays)
+  const float wm = fast_max(o.m);
+  const float ws = fast_sum(scaled(o, wm));
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = o;
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = Online{wm, ws};
   __syncthreads();
-  o = sm[0];
-  for (int i = 1; i < NT / 64; ++i) o = online_join(o, sm[i], c);
-  return o;
+  const Online x = sm[threadIdx.x % (NT / 64)];
+  const float m = fast_max(x.m);
+  return Online{m, fast_sum((threadIdx.x & 63) < NT / 64 ? scaled(x, m) : 0.f)};
 }
 // 2^(c (z - m)) of values z <= m as 2^(slope z + shift), in one fused step.  Where c m is so large that 1 beside it is nothing (or it has
 // no number: columns masked with the type's lowest value), a power of two takes the place of c, so that slope m is exact, the
@@ -95,8 +115,8 @@ __device__ __forceinline__ float row_lse(const Online& o, float tau) {
 // (a few hundred of 128256) and ranked by counting.
 // Sum of exponentials: against a shift that a wave keeps to itself and raises only where a chunk passes T (it is never below
 // T, so what does not pass cannot exceed it): per element one conversion, half a maximum, one fused step, the exponential and
-// one addition.  The first round has no T yet: each wave takes the k-th largest of its own 64 U chunk maxima, and the
-// largest of those serves all.
+// one addition.  The first round has no T yet: k chunks of one wave reach the k-th largest of its 64 U maxima, and k of all NW waves the
+// least of their (k / NW)-th largest; the larger of the two serves all.
 // Bound by memory: [8192, 128256] bf16, k = 32: 327 us, 6.4 TB/s (k = 1: 321, k = 128: 365).
 // ----------------------------------------------------------------------------------------------
 namespace {
@@ -145,6 +165,7 @@ __device__ __forceinline__ uint32_t cut_prefix(const uint64_t* list, int n, int 
   for (int i = 0; i < NI; ++i) key[i] = lane + 64 * i < n ? (uint32_t)(list[lane + 64 * i] >> 32) : 0u;
   uint32_t t = 0;
   left = n;
+#pragma unroll 1
   for (int bit = 31; bit >= 16; --bit) {
     const uint32_t u = t | (1u << bit);
     int c = 0;
@@ -154,7 +175,7 @@ __device__ __forceinline__ uint32_t cut_prefix(const uint64_t* list, int n, int 
   }
   return t;
 }
-__device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int lane) {
+__device__ __noinline__ ListCut list_cut(uint64_t* list, int n, int k, int lane) {
   int left = n;
   uint64_t t;
   if (n <= 128) {
@@ -167,6 +188,7 @@ __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int la
     t = (uint64_t)cut_prefix<16>(list, n, k, lane, left) << 32;
   } else {
     t = 0;
+#pragma unroll 1
     for (int bit = 63; bit >= 48; --bit) {
       const uint64_t u = t | (1ull << bit);
       int c = 0;
@@ -176,6 +198,7 @@ __device__ __forceinline__ ListCut list_cut(uint64_t* list, int n, int k, int la
   }
   const uint32_t key = (uint32_t)(t >> 32);
   if (left > k + list_slack(k))
+#pragma unroll 1
     for (int bit = 47; bit >= 0; --bit) {
       const uint64_t u = t | (1ull << bit);
       int c = 0;
@@ -200,11 +223,14 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
                                                          int32_t* __restrict__ ids, float* __restrict__ values,
                                                          float* __restrict__ lse) {
   constexpr int NW = NT / 64, ROUND = NT * U * 8;
-  constexpr int CAP = NT * U + kListKept > kListKept * 8 ? NT * U + kListKept : kListKept * 8;
+  // What the list may hold between rounds.  A block alone on its CU waits for every cut: only its last one, and those that the list's room
+  // asks for.
+  constexpr int KEPT = NT == 1024 ? 512 : kListKept;
+  constexpr int CAP = NT * U + KEPT > kListKept * 8 ? NT * U + KEPT : kListKept * 8;
   __shared__ uint64_t list[CAP];
   __shared__ uint32_t chunk_of[kListKept];
   __shared__ int added[3];
-  __shared__ uint32_t first_key, cut_key, top_key;
+  __shared__ uint32_t first_any, first_all, cut_key, top_key;
   __shared__ int cut_n, found_n;
   __shared__ Online sm[NW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -213,7 +239,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
   const float c = kLog2e / tau;
   const int last = (V - 1) / 8 * 8;                 // the last chunk: whole in memory, since rows are multiples of eight apart
   if (threadIdx.x < 3) added[threadIdx.x] = 0;
-  if (threadIdx.x == 3) { first_key = 0; found_n = 0; }
+  if (threadIdx.x == 3) { first_any = 0; first_all = ~0u; found_n = 0; }
   lds_barrier();
 
   Raw8Once<T> ring[D][U];                           // the next D rounds
@@ -247,9 +273,9 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
     }
   };
   int r = 0;                                        // the round, modulo 3
-  auto round = [&](Raw8Once<T> (&cur)[U], int base) {
+  auto round = [&](auto FIRST, Raw8Once<T> (&cur)[U], int base) {   // FIRST: whether this can be the row's first round
     const bool tail = base + ROUND > V;
-    if (base == 0) {
+    if (decltype(FIRST)::value && base == 0) {
       uint32_t key[U];
       float all = -INFINITY;
 #pragma unroll
@@ -261,18 +287,28 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
         key[u] = col < V ? order_key(cm) : 0u;
         all = fmaxf(all, cm);
       }
-      uint32_t t = 0;
+      // prefixes that k of the wave's chunks reach, and as many as make k of all waves together
+      const int share = (k + NW - 1) / NW;
+      uint32_t ta = 0, tb = 0;
+#pragma unroll 1
       for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t x = t | (1u << bit);
-        int count = 0;
+        const uint32_t xa = ta | (1u << bit), xb = tb | (1u << bit);
+        int na = 0, nb = 0;
 #pragma unroll
-        for (int u = 0; u < U; ++u) count += __popcll(__ballot(key[u] >= x));
-        if (count >= k) t = x;
+        for (int u = 0; u < U; ++u) {
+          na += __popcll(__ballot(key[u] >= xa));
+          nb += __popcll(__ballot(key[u] >= xb));
+        }
+        if (na >= k) ta = xa;
+        if (nb >= share) tb = xb;
       }
-      if (lane == 0 && t) atomicMax(&first_key, t);
-      raise(wave_max(all));
+      if (lane == 0) {
+        atomicMax(&first_any, ta);
+        atomicMin(&first_all, tb);
+      }
+      raise(fast_max(all));
       lds_barrier();
-      t = first_key;
+      const uint32_t t = max(first_any, first_all);
       if (t > 2) T_v = key_value(t - 2);            // k chunks have keys of at least t; two steps, for the two zeros
       raise(T_v);
     }
@@ -287,7 +323,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
       const bool pass = col < V && !(cm <= T_v);
       who[u] = __ballot(pass);
       top[u] = cm;
-      if (who[u] && __any(cm > m)) raise(wave_max(fmaxf(cm, m)));
+      if (who[u] && __any(cm > m)) raise(fast_max(cm));
       float part = 0.f;
       if (wide) {   // (as power_of, which takes registers that are not there)
 #pragma unroll
@@ -315,7 +351,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
     lds_barrier();
     n += added[r];
     if (threadIdx.x == 0) added[r == 0 ? 2 : r - 1] = 0;   // read by all before this barrier, used again behind the next
-    if (n > k + list_slack(k) || (base + ROUND >= V && n > k)) {
+    if (n > (NT == 1024 ? KEPT : k + list_slack(k)) || (base + ROUND >= V && n > k)) {
       if (wave == 0) {
         const ListCut cut = list_cut(list, n, k, lane);
         if (lane == 0) { cut_n = cut.n; cut_key = cut.key; }
@@ -329,14 +365,17 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
     load(cur, base + D * ROUND);
   };
   for (int base = 0; base < V; base += D * ROUND) {
+    round(std::true_type{}, ring[0], base);
 #pragma unroll
-    for (int d = 0; d < D; ++d)
-      if (base + d * ROUND < V) round(ring[d], base + d * ROUND);
+    for (int d = 1; d < D; ++d)
+      if (base + d * ROUND < V) round(std::false_type{}, ring[d], base + d * ROUND);
   }
 
   // the elements of the chunks left, of which k reach the last threshold
   const uint32_t least = n >= k && T_v == T_v ? order_key(T_v) : 0u;
   if (threadIdx.x < n) chunk_of[threadIdx.x] = ~(uint32_t)list[threadIdx.x];
+  s = fast_sum(s);                                  // (the shift is the wave's)
+  if (lane == 0) sm[wave] = Online{m, s};
   lds_barrier();
   for (int e = threadIdx.x; e < n * 8; e += NT) {
     const int col = (int)(chunk_of[e >> 3] * 8u) + (e & 7);
@@ -359,10 +398,12 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
     }
   }
   if (lse) {
-    const Online o = online_block<NT>(Online{m, s}, c, sm);
-    if (threadIdx.x == 0) {
+    lds_barrier();
+    if (wave == 0) {
+      const Online x = lane < NW ? sm[lane] : Online{-INFINITY, 0.f};
+      const float all = fast_max(x.m), sum = fast_sum(x.m == -INFINITY ? x.s : x.s * __builtin_amdgcn_exp2f((x.m - all) * c));
       const float top = key_value(top_key);         // -inf, +inf and NaN have no sum: the row's log-sum-exp is its largest element
-      lse[row] = fabsf(top) < INFINITY ? o.m / tau + logf(o.s) : top;
+      if (lane == 0) lse[row] = fabsf(top) < INFINITY ? all / tau + logf(sum) : top;
     }
   }
 }
@@ -440,11 +481,11 @@ __device__ __forceinline__ void teacher_load(Teacher& te, const TeacherRegs& r, 
   const bool any = __any(says);
   float L = r.lse;
   if (!args.tlse) {
-    m = wave_max(m);
+    m = fast_max(m);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < kTeacherPer; ++i) s += r.id[i] >= 0 && any ? expf(a[i] - m) : 0.f;
-    L = m + logf(wave_sum(s));
+    L = m + logf(fast_sum(s));
   }
   float mass = 0.f, ent = 0.f;
 #pragma unroll
@@ -457,8 +498,8 @@ __device__ __forceinline__ void teacher_load(Teacher& te, const TeacherRegs& r, 
     te.p[j] = p;
     te.z[j] = r.z[i];
   }
-  mass = wave_sum(mass);
-  ent = wave_sum(ent);
+  mass = fast_sum(mass);
+  ent = fast_sum(ent);
   if (lane == 0) { te.mass = mass; te.loss = ent; te.any = any ? 1 : 0; }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   float at[kTeacherPer] = {};
@@ -481,7 +522,7 @@ __device__ __forceinline__ float teacher_loss(const Teacher& te, int k, const On
     const int j = lane + 64 * i;
     if (j < k && te.p[j] != 0.f) x += te.p[j] * ((te.z[j] - o.m) / tau - log_s);
   }
-  return te.loss - wave_sum(x);
+  return te.loss - fast_sum(x);
 }
 
 // What a block knows of its row after the statistics, and what remains but for the dense part of the gradient: the loss, and the
@@ -607,7 +648,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
   extern __shared__ u32x4_t distill_row_lds[];                 // n_lds x NT chunks
   __shared__ Teacher te;
-  __shared__ float red[17];
+  __shared__ float red[NT / 64], sums[NT / 64];
   const size_t row = blockIdx.x;
   const T* zr = (const T*)a.z + row * (size_t)a.ldz;
   T* dr = (T*)a.dz + row * (size_t)a.ldz;
@@ -696,11 +737,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     m = chunk_max(buf[i], m);
   }
   for (int i = 0; i < n_lds; ++i) m = chunk_max(mine[i * NT], m);
-  m = wave_max(m);
+  m = fast_max(m);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
   __syncthreads();
-  m = red[0];
-  for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, red[i]);
+  m = fast_max(red[threadIdx.x % (NT / 64)]);
   const Power pw = power_of(m, c);
   float s = 0.f;
 #pragma unroll
@@ -709,7 +749,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     s += chunk_sum(buf[i], pw.slope, pw.shift);
   }
   for (int i = 0; i < n_lds; ++i) s += chunk_sum(mine[i * NT], pw.slope, pw.shift);
-  const Online o{m, block_sum(s, red)};
+  s = fast_sum(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  const Online o{m, fast_sum((threadIdx.x & 63) < NT / 64 ? sums[threadIdx.x & 63] : 0.f)};
   const RowGrad g = teacher_finish(te, a, row, masked, o, c, true);
   if (!g.keep) {
     const u32x4_t zero = {0u, 0u, 0u, 0u};
