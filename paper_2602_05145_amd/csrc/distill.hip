@@ -34,6 +34,7 @@ template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp(float v, float none) {
   return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
 }
+__device__ __forceinline__ float scalar(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }   // the same in every lane
 __device__ __forceinline__ float last_lane(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63)); }
 __device__ __forceinline__ float fast_max(float v) {
   v = fmaxf(v, dpp<0x111, 0xf>(v, -INFINITY));   // from 1, 2, 4 and 8 lanes below in a row of 16
@@ -115,8 +116,8 @@ __device__ __forceinline__ float row_lse(const Online& o, float tau) {
 // (a few hundred of 128256) and ranked by counting.
 // Sum of exponentials: against a shift that a wave keeps to itself and raises only where a chunk passes T (it is never below
 // T, so what does not pass cannot exceed it): per element one conversion, half a maximum, one fused step, the exponential and
-// one addition.  The first round has no T yet: k chunks of one wave reach the k-th largest of its 64 U maxima, and k of all NW waves the
-// least of their (k / NW)-th largest; the larger of the two serves all.
+// one addition.  The first round has no T yet: k chunks of one wave reach the k-th largest of its maxima, and k of several waves the least
+// of their largest, second largest ...: what is enough for k.
 // Bound by memory: [8192, 128256] bf16, k = 32: 327 us, 6.4 TB/s (k = 1: 321, k = 128: 365).
 // ----------------------------------------------------------------------------------------------
 namespace {
@@ -215,6 +216,25 @@ __device__ __noinline__ ListCut list_cut(uint64_t* list, int n, int k, int lane)
   return ListCut{out, key};
 }
 
+// How many of a list's n <= NT pairs are larger than pair i, which is the thread's own: as many neighbouring threads share a pair as there
+// are threads for, up to 16.
+template <int CTRL>
+__device__ __forceinline__ int dpp_int(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, false); }
+template <int NT>
+__device__ __forceinline__ int list_rank(const uint64_t* list, int n, int& i, uint64_t& pair) {
+  const int log = n <= NT / 16 ? 4 : n <= NT / 8 ? 3 : n <= NT / 4 ? 2 : n <= NT / 2 ? 1 : 0;
+  i = (int)threadIdx.x >> log;
+  pair = i < n ? list[i] : ~0ull;
+  int rank = 0;
+#pragma unroll 4
+  for (int j = threadIdx.x & ((1 << log) - 1); j < n; j += 1 << log) rank += list[j] > pair ? 1 : 0;
+  if (log > 0) rank += dpp_int<0xB1>(rank);    // the neighbour, the neighbouring pair, the other four, the other eight
+  if (log > 1) rank += dpp_int<0x4E>(rank);
+  if (log > 2) rank += dpp_int<0x141>(rank);
+  if (log > 3) rank += dpp_int<0x140>(rank);
+  return rank;
+}
+
 }  // namespace
 
 // (256 threads in 89 registers, five blocks on a CU: 365 us where seven take 327)
@@ -223,20 +243,19 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
                                                          int32_t* __restrict__ ids, float* __restrict__ values,
                                                          float* __restrict__ lse) {
   constexpr int NW = NT / 64, ROUND = NT * U * 8;
-  // What the list may hold between rounds.  A block alone on its CU waits for every cut: only its last one, and those that the list's room
-  // asks for.
-  constexpr int KEPT = NT == 1024 ? 512 : kListKept;
-  constexpr int CAP = NT * U + KEPT > kListKept * 8 ? NT * U + KEPT : kListKept * 8;
+  constexpr bool RANKS = NT > 256;   // cut by ranks, by the whole block at once: less waiting, more work
+  constexpr int CAP = NT * U + kListKept > kListKept * 8 ? NT * U + kListKept : kListKept * 8;
   __shared__ uint64_t list[CAP];
   __shared__ uint32_t chunk_of[kListKept];
   __shared__ int added[3];
   __shared__ uint32_t first_any, first_all, cut_key, top_key;
+  __shared__ float first[NW];
   __shared__ int cut_n, found_n;
   __shared__ Online sm[NW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const size_t row = blockIdx.x;
   const T* zr = z + row * (size_t)ldz;
-  const float c = kLog2e / tau;
+  const float c = scalar(kLog2e / tau);
   const int last = (V - 1) / 8 * 8;                 // the last chunk: whole in memory, since rows are multiples of eight apart
   if (threadIdx.x < 3) added[threadIdx.x] = 0;
   if (threadIdx.x == 3) { first_any = 0; first_all = ~0u; found_n = 0; }
@@ -257,7 +276,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
   float shift = 0.f;                                // -c m, 0 before any number
   bool wide = false;                                // whether that is too large to be added to
   auto raise = [&](float to) {                      // the same in the whole wave
-    to = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(to)));
+    to = scalar(to);
     if (to > m) {
       s *= m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);   // (before any number the sum is 0, or NaN)
       m = to;
@@ -277,7 +296,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
     const bool tail = base + ROUND > V;
     if (decltype(FIRST)::value && base == 0) {
       uint32_t key[U];
-      float all = -INFINITY;
+      float all = -INFINITY;                        // the lane's largest number
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int col = (threadIdx.x + u * NT) * 8;
@@ -287,29 +306,51 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
         key[u] = col < V ? order_key(cm) : 0u;
         all = fmaxf(all, cm);
       }
-      // prefixes that k of the wave's chunks reach, and as many as make k of all waves together
       const int share = (k + NW - 1) / NW;
-      uint32_t ta = 0, tb = 0;
+      float t = fast_max(all);
+      raise(t);
+      if constexpr (RANKS) {
+        // `share` lanes of a wave reach its share-th largest, and k chunks that of enough waves
+        const int waves = (k + share - 1) / share;
+        float left = all;
 #pragma unroll 1
-      for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t xa = ta | (1u << bit), xb = tb | (1u << bit);
-        int na = 0, nb = 0;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          na += __popcll(__ballot(key[u] >= xa));
-          nb += __popcll(__ballot(key[u] >= xb));
+        for (int i = 1; i < share; ++i) {
+          if (lane == __builtin_ctzll(__ballot(left == t) | (1ull << 63))) left = -INFINITY;
+          t = fast_max(left);
         }
-        if (na >= k) ta = xa;
-        if (nb >= share) tb = xb;
+        if (lane == 0) first[wave] = t;
+        lds_barrier();
+        const float mine = first[lane % NW];
+        int rank = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) rank += first[i] > mine || (first[i] == mine && i < lane) ? 1 : 0;
+        const uint64_t at = __ballot(lane < NW && rank == waves - 1);
+        t = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), __builtin_ctzll(at | (1ull << 63))));
+        if (at && t > -INFINITY) T_v = scalar(key_value(order_key(t) - 2));   // (two steps below: the zeros are one)
+      } else {
+        // prefixes that k of the wave's chunks reach, and as many as make k of all waves together (the form above takes five registers
+        // more than seven blocks on a CU have: [8192, 128256] bf16 387 us where this takes 325)
+        uint32_t ta = 0, tb = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 16; --bit) {
+          const uint32_t xa = ta | (1u << bit), xb = tb | (1u << bit);
+          int na = 0, nb = 0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            na += __popcll(__ballot(key[u] >= xa));
+            nb += __popcll(__ballot(key[u] >= xb));
+          }
+          if (na >= k) ta = xa;
+          if (nb >= share) tb = xb;
+        }
+        if (lane == 0) {
+          atomicMax(&first_any, ta);
+          atomicMin(&first_all, tb);
+        }
+        lds_barrier();
+        const uint32_t reached = max(first_any, first_all);
+        if (reached > 2) T_v = scalar(key_value(reached - 2));
       }
-      if (lane == 0) {
-        atomicMax(&first_any, ta);
-        atomicMin(&first_all, tb);
-      }
-      raise(fast_max(all));
-      lds_barrier();
-      const uint32_t t = max(first_any, first_all);
-      if (t > 2) T_v = key_value(t - 2);            // k chunks have keys of at least t; two steps, for the two zeros
       raise(T_v);
     }
     uint64_t who[U];
@@ -349,16 +390,28 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
       }
     }
     lds_barrier();
-    n += added[r];
+    n += __builtin_amdgcn_readfirstlane(added[r]);
     if (threadIdx.x == 0) added[r == 0 ? 2 : r - 1] = 0;   // read by all before this barrier, used again behind the next
-    if (n > (NT == 1024 ? KEPT : k + list_slack(k)) || (base + ROUND >= V && n > k)) {
-      if (wave == 0) {
-        const ListCut cut = list_cut(list, n, k, lane);
-        if (lane == 0) { cut_n = cut.n; cut_key = cut.key; }
+    if (n > k + list_slack(k) || (base + ROUND >= V && n > k)) {
+      if (!RANKS || n > NT) {
+        if (wave == 0) {
+          const ListCut cut = list_cut(list, n, k, lane);
+          if (lane == 0) { cut_n = cut.n; cut_key = cut.key; }
+        }
+        lds_barrier();
+        n = __builtin_amdgcn_readfirstlane(cut_n);
+        T_v = scalar(key_value(cut_key));
       }
-      lds_barrier();
-      n = cut_n;
-      T_v = key_value(cut_key);
+      if (RANKS && n > k) {
+        int i;
+        uint64_t pair;
+        const int rank = list_rank<NT>(list, n, i, pair);
+        lds_barrier();
+        if (i < n && rank < k) list[rank] = pair;
+        lds_barrier();
+        n = k;
+        T_v = scalar(key_value((uint32_t)(list[k - 1] >> 32)));
+      }
       raise(T_v);
     }
     r = r == 2 ? 0 : r + 1;
@@ -386,15 +439,23 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
   }
   lds_barrier();
   const int found = found_n;
-  for (int i = threadIdx.x; i < found; i += NT) {
-    const uint64_t p = list[i];
-    int rank = 0;
+  auto put = [&](int rank, uint64_t pair) {
+    ids[row * (size_t)k + rank] = (int32_t)~(uint32_t)pair;
+    values[row * (size_t)k + rank] = key_value((uint32_t)(pair >> 32));
+    if (rank == 0) top_key = (uint32_t)(pair >> 32);
+  };
+  if (RANKS && found <= NT) {
+    int i;
+    uint64_t pair;
+    const int rank = list_rank<NT>(list, found, i, pair);
+    if (i < found && rank < k) put(rank, pair);   // (threads that share a pair write the same)
+  } else {
+    for (int i = threadIdx.x; i < found; i += NT) {
+      const uint64_t pair = list[i];
+      int rank = 0;
 #pragma unroll 4
-    for (int j = 0; j < found; ++j) rank += list[j] > p ? 1 : 0;
-    if (rank < k) {
-      ids[row * (size_t)k + rank] = (int32_t)~(uint32_t)p;
-      values[row * (size_t)k + rank] = key_value((uint32_t)(p >> 32));
-      if (rank == 0) top_key = (uint32_t)(p >> 32);
+      for (int j = 0; j < found; ++j) rank += list[j] > pair ? 1 : 0;
+      if (rank < k) put(rank, pair);
     }
   }
   if (lse) {
