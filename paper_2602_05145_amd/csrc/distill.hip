@@ -474,11 +474,11 @@ hipError_t launch_topk_logits(int64_t rows, int V, const void* z, int64_t ldz, i
   if (rows <= 0) return hipSuccess;
   ProfScope ps("topk_logits", 0, (double)rows * ((double)V * dtype_size(dtype) + 8.0 * k), s);
   const dim3 grid((unsigned)rows);
-  // Up to a row per CU, all of a CU's threads on it, and four rounds requested at a time; two rows, half of them; beyond, four waves a row
-  // (us, 1024 / 512 / 256 threads, [rows, 128256] bf16, k = 32: 61 rows 27 / 29 / 43, 256 30 / 32 / 44, 512 57 / 39 / 49,
-  // 1024 108 / 72 / 59).
+  // Up to half a row per CU, as many threads as share a CU on it, and four rounds requested at a time; up to two, half of them; beyond, four
+  // waves a row (us, 1024 / 512 / 256 threads, [rows, 128256] bf16, k = 32: 61 rows 20.7 / 22.6 / 37.7, 256 25.7 / 24.2 / 39.8, 384 45.8 / 31.8 / 42.9,
+  // 512 49.5 / 32.7 / 43.8, 768 72.8 / 50.4 / 48.8, 1024 95.9 / 60.5 / 55.1).
   // (Eight blocks a CU in fp32, without a round requested ahead, against seven with one: [1999, 32001] 57 / 61 us; bf16 [8192, 128256] 334 / 326.)
-  const int nt = rows <= 256 ? 1024 : rows <= 512 ? 512 : 256;
+  const int nt = rows <= 128 ? 1024 : rows <= 512 ? 512 : 256;
 #define TIDE_TOPK(T, NT, U, D) hipLaunchKernelGGL((topk_logits_kernel<T, NT, U, D>), grid, dim3(NT), 0, s, (const T*)z, ldz, V, k, tau, ids, values, lse)
   if (dtype == kBF16) {
     if (nt == 1024) TIDE_TOPK(bf16_t, 1024, 4, 4);

@@ -1607,53 +1607,52 @@ hipError_t launch_gemm_adam(const GemmArgs& a, const AdamTarget& t, hipStream_t 
 }
 
 namespace {
-template <int BM, int BN, int LM>
+template <int BM, int LM>
 hipError_t launch_lm_tiles(MfmaLmParams& p, hipStream_t s) {
   p.tiles_m = (p.M + BM - 1) / BM;
-  p.tiles_n = (p.N + BN - 1) / BN;
-  const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(2 * BN);
-  if constexpr (BM == BN) {
+  p.tiles_n = (p.N + 255) / 256;
+  const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(512);
+  if constexpr (BM == 256) {
     if (!whole_slabs(p)) {
-      hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, BN, false, LM>), grid, blk, 0, s, p);
+      hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, 256, false, LM>), grid, blk, 0, s, p);
       return hipGetLastError();
     }
   }
-  hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, BN, true, LM>), grid, blk, 0, s, p);
+  hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, 256, true, LM>), grid, blk, 0, s, p);
   return hipGetLastError();
 }
-// Tiles of the head's logits: the cheapest by the costs that all products are planned with, of whole tiles only (and with a ragged K of
-// the squares); of the heights, those that the others come close to.
-LaunchPlan plan_lm(const GemmArgs& a) {
-  LaunchPlan best{128, 128, kSplitNone, {1, 0, 0}, {0, 0, 0}};
+// Height of the tiles of the head's logits: the cheapest by the costs that all products are planned with (a ragged K takes 256).  Forward, us,
+// 128 / 192 / 256 rows, width 2048, 32000 columns: 16 rows 41 / 47 / 54, 128 48 / 51 / 61, 300 73 / 57 / 64, 600 of 700 108 / 96 / 108, 1415 of 1665
+// 194 / 181 / 171; width 4096, 128256 columns: 128 rows 212 / 226 / 248, 400 493 / 486 / 433, 3400 of 3999 3375 / 2973 / 2878 (squares of 128
+// 45, 49, 78, 108, 204, 234, 548, 3753: nowhere the fastest).
+int lm_height(const GemmArgs& a) {
+  if (a.K % 64) return 256;
+  int best = 256;
   int64_t least = -1;
-  for (const int BM : {128, 192, 256, 0}) {
-    const LaunchPlan lp{BM ? BM : 128, BM ? 256 : 128, kSplitNone, {1, 0, 0}, {0, 0, 0}};
-    if (lp.BM != lp.BN && a.K % 64) continue;
-    if (BM == 0 && tile_count(a.M, a.N, 256) >= 4096) continue;   // (statistics of half as many columns each: callers hold memory for those of 256 then)
+  for (const int BM : {256, 192, 128}) {
     int64_t t = 0;
-    for (int share = 10; share <= 20; ++share) t += launch_time(a, lp, std::max<int64_t>(1, a.M * share / 20));
-    if (least < 0 || t < least) { least = t; best = lp; }
+    for (int share = 10; share <= 20; ++share)
+      t += launch_time(a, LaunchPlan{BM, 256, kSplitNone, {1, 0, 0}, {0, 0, 0}}, std::max<int64_t>(1, a.M * share / 20));
+    if (least < 0 || t < least) { least = t; best = BM; }
   }
   return best;
 }
 template <int LM>
 hipError_t launch_lm(const GemmArgs& a, const LmTarget& t, hipStream_t s) {
   if (a.layout != kNT || !gemm_mfma_supported(a) || a.A2 || (LM == kLmGrad && (a.N % 8 || a.ldc % 8 || ((uintptr_t)a.C & 15)))) return hipErrorInvalidValue;
-  const LaunchPlan lp = plan_lm(a);
+  const int BM = lm_height(a);
   MfmaLmParams p;
-  fill_params(p, a, lp);
+  fill_params(p, a, LaunchPlan{BM, 256, kSplitNone, {1, 0, 0}, {0, 0, 0}});
   p.lm = t;
   ProfScope ps(LM == kLmStats ? "lm_ce_stats" : "lm_ce_grad", 2.0 * (double)a.M * (double)a.N * (double)a.K,
                2.0 * (double)a.K * ((double)a.M + (double)a.N) + (LM == kLmGrad ? 2.0 * (double)a.M * (double)a.N : 0.0), s);
   if (a.m_dev) prof_dynamic(a.m_dev, a.m_off, a.M);
-  if (lp.BN == 128) return launch_lm_tiles<128, 128, LM>(p, s);
-  if (lp.BM == 128) return launch_lm_tiles<128, 256, LM>(p, s);
-  if (lp.BM == 192) return launch_lm_tiles<192, 256, LM>(p, s);
-  return launch_lm_tiles<256, 256, LM>(p, s);
+  if (BM == 128) return launch_lm_tiles<128, LM>(p, s);
+  if (BM == 192) return launch_lm_tiles<192, LM>(p, s);
+  return launch_lm_tiles<256, LM>(p, s);
 }
 }  // namespace
 
-int gemm_lm_stat_columns(const GemmArgs& a) { return plan_lm(a).BN; }
 hipError_t launch_gemm_lm_stats(const GemmArgs& a, const LmTarget& t, hipStream_t s) { return launch_lm<kLmStats>(a, t, s); }
 hipError_t launch_gemm_lm_grad(const GemmArgs& a, const LmTarget& t, hipStream_t s) { return launch_lm<kLmGrad>(a, t, s); }
 

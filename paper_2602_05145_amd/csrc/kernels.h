@@ -69,14 +69,14 @@ bool gemm_adam_group_pays(int64_t rows);
 hipError_t launch_gemm_adam_group(const GemmArgs* a, const AdamTarget* t, int n, hipStream_t s);
 hipError_t launch_gemm_group(const GemmArgs* a, int n, hipStream_t s);  // independent products, in one launch where small
 // The LM head's logits z = y W^T (NT, bf16) that are not kept.  Forward: part[t * part_ld + row] = the maximum of z and the sum of
-// exp(z - that) over the t-th gemm_lm_stat_columns columns, label[row] = z[row, tokens[row]] where the launch's columns hold it.
+// exp(z - that) over the t-th kLmColumns columns, label[row] = z[row, tokens[row]] where the launch's columns hold it.
 // Backward: C = weight (exp(z - lse) - [column == token]) in bf16, for columns n0 + c of the vocabulary; the first `zero` columns get 0.
 struct LmRow { float shift, weight; int token; float lse; };   // shift = -lse / ln 2
+constexpr int kLmColumns = 256;
 struct LmTarget {
   const int32_t* tokens; float2* part; int64_t part_ld; float* label;
   const LmRow* rows; int n0, zero;
 };
-int gemm_lm_stat_columns(const GemmArgs& a);
 hipError_t launch_gemm_lm_stats(const GemmArgs& a, const LmTarget& t, hipStream_t s);
 hipError_t launch_gemm_lm_grad(const GemmArgs& a, const LmTarget& t, hipStream_t s);
 // fp32, both sizes of the MLP's activations at once.  Forward: gate and up products and h = silu(gate) up in one launch; backward:

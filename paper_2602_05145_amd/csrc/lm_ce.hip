@@ -79,8 +79,7 @@ LmCePlan make_plan(int64_t rows, int64_t V, int64_t d, int dtype) {
   p.tokens_c = take(T * 4);
   p.rows_c = take(T * sizeof(LmRow));
   p.y_c = take(T * d * es);
-  // (statistics of 128 columns each are fewer bytes than the whole vocabulary's dz, which is what the array holds where tiles are that small)
-  p.z = take(std::max((size_t)piece_elems(rows, V, dtype) * es, dtype == kBF16 ? T * (size_t)((V + 255) / 256) * sizeof(float2) : 0));
+  p.z = take(std::max((size_t)piece_elems(rows, V, dtype) * es, dtype == kBF16 ? T * (size_t)((V + kLmColumns - 1) / kLmColumns) * sizeof(float2) : 0));
   p.acc = pc.count > 1 && dtype == kBF16 ? take(T * d * 4) : 0;
   p.dy_c = take(T * d * es);
   if (dtype == kF32 || pc.count == 1) p.acc = p.dy_c;
@@ -335,7 +334,7 @@ hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s) {
   if (a.dtype == kBF16) {
     GemmArgs g = c.logits(Piece{0, a.V, 0});
     g.ldc = a.V;
-    const int columns = gemm_lm_stat_columns(g), tiles = (int)((a.V + columns - 1) / columns);
+    const int tiles = (int)((a.V + kLmColumns - 1) / kLmColumns);
     float* label = c.at<float>(c.p.rows_c);
     LmTarget t{c.at<int32_t>(c.p.tokens_c), c.at<float2>(c.p.z), a.rows, label, nullptr, 0, 0};
     LM_TRY(launch_gemm_lm_stats(g, t, s));
