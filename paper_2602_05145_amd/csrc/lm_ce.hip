@@ -14,7 +14,7 @@
 
 #include "kernels.h"
 #include "prof.h"
-#include "tide_common.h"
+#include "row_stats.h"
 
 namespace tide {
 
@@ -194,32 +194,24 @@ __global__ __launch_bounds__(256) void lm_begin_kernel(LmBegin a) {
 __global__ __launch_bounds__(256) void lm_stats_kernel(const float* __restrict__ z, int64_t ldz, int n0, int n, const int32_t* __restrict__ tokens,
                                                        const int* __restrict__ cnt, RowState* __restrict__ st, int last, const int32_t* __restrict__ kept_idx,
                                                        float* __restrict__ lse, float* __restrict__ loss_rows) {
-  __shared__ float sm[4];
-  __shared__ float red[17];
+  __shared__ Online sm[4];
   const int row = blockIdx.x;
   if (row >= *cnt) return;
   const float* zr = z + (size_t)row * ldz;
-  float m = -INFINITY;
-  for (int c = threadIdx.x; c < n; c += 256) m = fmaxf(m, zr[c]);
-  m = wave_max(m);
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  const RowState o = st[row];
-  m = fmaxf(m, o.m);
-  float s = 0.f;
-  for (int c = threadIdx.x; c < n; c += 256) s += expf(zr[c] - m);
-  s = block_sum(s, red);
+  Online x = online_block<256>(row_stats<float, 256>(zr, n, kLog2e), kLog2e, sm);
   if (threadIdx.x == 0) {
+    const RowState o = st[row];
     const int t = tokens[row] - n0;
-    const RowState x{m, (o.m == -INFINITY ? o.s : o.s * expf(o.m - m)) + s, t >= 0 && t < n ? zr[t] : o.z};
+    const float m = fmaxf(x.m, o.m);
+    const float s = (x.m == -INFINITY ? x.s : x.s * expf(x.m - m)) + (o.m == -INFINITY ? o.s : o.s * expf(o.m - m));
+    const RowState all{m, s, t >= 0 && t < n ? zr[t] : o.z};
     if (last) {
-      const float log_s = logf(x.s);
+      const float log_s = logf(all.s);
       const int at = kept_idx[row];
-      lse[at] = x.m + log_s;
-      loss_rows[at] = log_s + (x.m - x.z);
+      lse[at] = all.m + log_s;
+      loss_rows[at] = log_s + (all.m - all.z);
     } else {
-      st[row] = x;
+      st[row] = all;
     }
   }
 }
@@ -255,14 +247,21 @@ __global__ __launch_bounds__(256) void lm_join_kernel(const float2* __restrict__
   }
 }
 
-// fp32: a piece's logits become their gradient
+// fp32: a piece's logits become their gradient (and what is behind a row's last column up to the next multiple of eight, something)
 __global__ __launch_bounds__(256) void lm_grad_kernel(float* z, int64_t ldz, int n0, int n, const int* __restrict__ cnt, const LmRow* __restrict__ rows) {
   const int row = blockIdx.x;
   if (row >= *cnt) return;
   const LmRow o = rows[row];
   const int t = o.token - n0;
   float* zr = z + (size_t)row * ldz;
-  for (int c = threadIdx.x; c < n; c += 256) zr[c] = o.weight * (expf(zr[c] - o.lse) - (c == t ? 1.f : 0.f));
+  const int first = (blockIdx.y * 256 + threadIdx.x) * 8, step = (int)gridDim.y * 2048;
+  for (int c = first; c < n; c += step) {
+    float v[8];
+    ld8(zr, c, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = o.weight * (expf(v[j] - o.lse) - (c + j == t ? 1.f : 0.f));
+    st8(zr, c, v);
+  }
 }
 
 // compact rows back to their places, zeros elsewhere
@@ -371,7 +370,7 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
       LM_TRY(launch_gemm(c.logits(q), s));
       ProfScope ps("lm_ce_grad_fp32", 0, 8.0 * (double)a.rows * q.n, s);
       prof_dynamic(c.cnt(), 0, a.rows);
-      hipLaunchKernelGGL(lm_grad_kernel, dim3((unsigned)a.rows), dim3(256), 0, s, c.at<float>(c.p.z), ld, (int)q.n0, (int)q.n, c.cnt(), rows);
+      hipLaunchKernelGGL(lm_grad_kernel, dim3((unsigned)a.rows, (unsigned)std::min<int64_t>((q.n + 2047) / 2048, 64)), dim3(256), 0, s, c.at<float>(c.p.z), ld, (int)q.n0, (int)q.n, c.cnt(), rows);
       LM_TRY(hipGetLastError());
     }
     GemmArgs g = product(kNN, a.rows, a.d, q.n, c.ws + c.p.z, ld, c.piece_w(q), a.d, c.ws + c.p.acc, a.d, a.dtype, to_acc ? kF32 : a.dtype);

@@ -1,0 +1,92 @@
+// Statistics of a softmax over rows of thousands of columns: the maximum and the sum of exponentials beside it, kept per lane, joined over
+// a wave and a block.
+#pragma once
+#include "tide_common.h"
+
+namespace tide {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Maximum and sum over a wave on the vector unit alone (a shuffle through LDS takes ten times as long, and a row's few blocks wait for each);
+// every lane gets the result.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float v, float none) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float scalar(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }   // the same in every lane
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63)); }
+__device__ __forceinline__ float fast_max(float v) {
+  v = fmaxf(v, dpp<0x111, 0xf>(v, -INFINITY));   // from 1, 2, 4 and 8 lanes below in a row of 16
+  v = fmaxf(v, dpp<0x112, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x114, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x118, 0xf>(v, -INFINITY));
+  v = fmaxf(v, dpp<0x142, 0xa>(v, -INFINITY));   // the row below's last lane, in rows 1 and 3; then the lower half's, in the upper
+  v = fmaxf(v, dpp<0x143, 0xc>(v, -INFINITY));
+  return last_lane(v);
+}
+__device__ __forceinline__ float fast_sum(float v) {
+  v += dpp<0x111, 0xf>(v, 0.f);
+  v += dpp<0x112, 0xf>(v, 0.f);
+  v += dpp<0x114, 0xf>(v, 0.f);
+  v += dpp<0x118, 0xf>(v, 0.f);
+  v += dpp<0x142, 0xa>(v, 0.f);
+  v += dpp<0x143, 0xc>(v, 0.f);
+  return last_lane(v);
+}
+
+// Running (max, sum of 2^(c (z - max))) over eight more values.  The difference comes first: it is 0 for the largest value whatever
+// that is, also where c times it has no number (columns masked with the type's lowest value).
+struct Online { float m, s; };
+__device__ __forceinline__ void online_add8(Online& o, const float (&v)[8], float c) {
+  float cm = v[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) cm = fmaxf(cm, v[j]);
+  const float nm = fmaxf(o.m, cm);
+  const float sh = nm == -INFINITY ? 0.f : nm;      // nothing but -inf so far: every term is 0
+  float part = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f((v[j] - sh) * c);
+  o.s = (o.m == -INFINITY ? o.s : o.s * __builtin_amdgcn_exp2f((o.m - nm) * c)) + part;   // (before any number: 0, or NaN)
+  o.m = nm;
+}
+// of a block of NT threads; every thread gets the result.  sm: NT / 64 pairs.  Two barriers.
+template <int NT>
+__device__ __forceinline__ Online online_block(const Online& o, float c, Online* sm) {
+  auto scaled = [&](const Online& x, float m) { return x.m == -INFINITY ? x.s : x.s * __builtin_amdgcn_exp2f((x.m - m) * c); };   // (a NaN in the sum stays)
+  const float wm = fast_max(o.m);
+  const float ws = fast_sum(scaled(o, wm));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = Online{wm, ws};
+  __syncthreads();
+  const Online x = sm[threadIdx.x % (NT / 64)];
+  const float m = fast_max(x.m);
+  return Online{m, fast_sum((threadIdx.x & 63) < NT / 64 ? scaled(x, m) : 0.f)};
+}
+
+// Of a thread of a block of NT, over columns 0 .. n of a row in memory, four chunks requested at a time.  The row is 16-byte aligned and what
+// is behind its last column up to the next multiple of eight can be read.
+template <typename T, int NT>
+__device__ __forceinline__ Online row_stats(const T* zr, int V, float c) {
+  constexpr int U = sizeof(T) == 2 ? 4 : 2, STEP = NT * 8;
+  const int last = (V - 1) / 8 * 8;
+  Online o{-INFINITY, 0.f};
+  for (int base = 0; base < V; base += U * STEP) {
+    Raw8<T> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u].load(zr, (size_t)min(base + u * STEP + (int)threadIdx.x * 8, last));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = base + u * STEP + threadIdx.x * 8;
+      float v[8];
+      raw[u].get(v);
+      if (base + U * STEP > V) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = col + j < V ? v[j] : -INFINITY;
+      }
+      online_add8(o, v, c);
+    }
+  }
+  return o;
+}
+
+}  // namespace tide
