@@ -80,21 +80,6 @@ __device__ __forceinline__ float max8(const float (&v)[8]) {
   const float m = max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), v[6]);
   return max3(m, v[7], v[7]);
 }
-template <typename T> struct Raw8Once : Raw8<T> {   // loads past the caches: nothing is read again
-  __device__ __forceinline__ void load_once(const T* p, size_t i) {
-    typedef unsigned u32x4_nt __attribute__((ext_vector_type(4)));
-    const u32x4_nt* q = reinterpret_cast<const u32x4_nt*>(p + i);
-    if constexpr (sizeof(T) == 2) {
-      const u32x4_nt x = __builtin_nontemporal_load(q);
-      this->a = make_uint4(x.x, x.y, x.z, x.w);
-    } else {
-      const u32x4_nt x = __builtin_nontemporal_load(q), y = __builtin_nontemporal_load(q + 1);
-      this->a = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
-      this->b = make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w));
-    }
-  }
-};
-
 // chunks that a list may hold at the start of a round beyond the k that it needs
 __host__ __device__ constexpr int list_slack(int k) { return 16 + k / 4; }
 constexpr int kListKept = kMaxTeacher + list_slack(kMaxTeacher);
@@ -608,7 +593,7 @@ __global__ __launch_bounds__(512) void distill_kernel(DistillArgs a) {
     teacher_fetch(regs, a, row, threadIdx.x);
     teacher_logits(regs, zr, a.V);
   }
-  Online o = row_stats<T, NT>(zr, a.V, c);
+  Online o = row_stats<T, NT, !GRAD>(zr, a.V, c);
   if (threadIdx.x < 64) teacher_load(te, regs, a, threadIdx.x);
   o = online_block<NT>(o, c, sm);
   const RowGrad g = teacher_finish(te, a, row, masked, o, c, GRAD);

@@ -63,17 +63,35 @@ __device__ __forceinline__ Online online_block(const Online& o, float c, Online*
   return Online{m, fast_sum((threadIdx.x & 63) < NT / 64 ? scaled(x, m) : 0.f)};
 }
 
+template <typename T> struct Raw8Once : Raw8<T> {   // loads past the caches: nothing is read again
+  __device__ __forceinline__ void load_once(const T* p, size_t i) {
+    typedef unsigned u32x4_nt __attribute__((ext_vector_type(4)));
+    const u32x4_nt* q = reinterpret_cast<const u32x4_nt*>(p + i);
+    if constexpr (sizeof(T) == 2) {
+      const u32x4_nt x = __builtin_nontemporal_load(q);
+      this->a = make_uint4(x.x, x.y, x.z, x.w);
+    } else {
+      const u32x4_nt x = __builtin_nontemporal_load(q), y = __builtin_nontemporal_load(q + 1);
+      this->a = make_float4(__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w));
+      this->b = make_float4(__uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w));
+    }
+  }
+};
+
 // Of a thread of a block of NT, over columns 0 .. n of a row in memory, four chunks requested at a time.  The row is 16-byte aligned and what
-// is behind its last column up to the next multiple of eight can be read.
-template <typename T, int NT>
+// is behind its last column up to the next multiple of eight can be read.  ONCE: it is not read again.
+template <typename T, int NT, bool ONCE = false>
 __device__ __forceinline__ Online row_stats(const T* zr, int V, float c) {
   constexpr int U = sizeof(T) == 2 ? 4 : 2, STEP = NT * 8;
   const int last = (V - 1) / 8 * 8;
   Online o{-INFINITY, 0.f};
   for (int base = 0; base < V; base += U * STEP) {
-    Raw8<T> raw[U];
+    Raw8Once<T> raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u].load(zr, (size_t)min(base + u * STEP + (int)threadIdx.x * 8, last));
+    for (int u = 0; u < U; ++u) {
+      const size_t at = (size_t)min(base + u * STEP + (int)threadIdx.x * 8, last);
+      if constexpr (ONCE) raw[u].load_once(zr, at); else raw[u].load(zr, at);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int col = base + u * STEP + threadIdx.x * 8;

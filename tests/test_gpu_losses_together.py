@@ -63,13 +63,13 @@ def test_a_step_against_autograd_in_64_bits(dtype):
     ce_dy, ce_dw = torch.autograd.grad(ce.sum() * p.scale, (y, w))
     loose = 2e-2 if dtype == "bf16" else 1e-5         # (the distillation's logits are stored in the mode's type)
     for got, want in ((p.loss, kd), (p.ce_loss, ce)):
-        assert float((got.double() - want).abs().max()) <= loose * (1 + float(want.detach().abs().max()))
+        assert float((got.double() - want.detach()).abs().max()) <= loose * (1 + float(want.detach().abs().max()))
     for got, want in ((p.dy, kd_dy), (p.dw, kd_dw), (p.ce_dy, ce_dy), (p.ce_dw, ce_dw)):
         assert cosine(to_host(got), want.detach().cpu().numpy()) > (0.9998 if dtype == "bf16" else 1 - 1e-9)
-        assert float((got.double() - want).norm() / want.norm()) < (1e-2 if dtype == "bf16" else 1e-5)
+        assert float((got.double() - want.detach()).norm() / want.norm()) < (1e-2 if dtype == "bf16" else 1e-5)
 
 
-@pytest.mark.parametrize("dtype,vocab", [("fp32", 3000), ("bf16", 3000), ("bf16", 40000)])
+@pytest.mark.parametrize("dtype,vocab", [("fp32", 3000), ("bf16", 3000), ("bf16", 40000), ("fp32", 40000), ("bf16", 128256), ("bf16", 140000)])
 def test_captured_and_replayed(dtype, vocab):
     """Every replay, with new inputs and eager work between them, gives the eager call's bits; two captured programs do not meet."""
     progs = [Program(dtype, vocab=vocab, seed=s) for s in (1, 2)]
@@ -83,7 +83,7 @@ def test_captured_and_replayed(dtype, vocab):
         with torch.cuda.graph(g, stream=side):
             p.step()
         graphs.append(g)
-    for turn in range(4):
+    for turn in range(3):
         for i, p in enumerate(progs):
             q = Program(dtype, vocab=vocab, seed=10 * turn + i)
             p.y.copy_(q.y)
