@@ -1621,11 +1621,13 @@ hipError_t launch_lm_tiles(MfmaLmParams& p, hipStream_t s) {
   hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, 256, true, LM>), grid, blk, 0, s, p);
   return hipGetLastError();
 }
-// Height of the tiles of the head's logits: the cheapest by the costs that all products are planned with (a ragged K takes 256).  Forward, us,
-// 128 / 192 / 256 rows, width 2048, 32000 columns: 16 rows 41 / 47 / 54, 128 48 / 51 / 61, 300 73 / 57 / 64, 600 of 700 108 / 96 / 108, 1415 of 1665
-// 194 / 181 / 171; width 4096, 128256 columns: 128 rows 212 / 226 / 248, 400 493 / 486 / 433, 3400 of 3999 3375 / 2973 / 2878 (squares of 128
-// 45, 49, 78, 108, 204, 234, 548, 3753: nowhere the fastest).
-int lm_height(const GemmArgs& a) {
+// Height of the tiles of the head's logits: the cheapest by the costs that all products are planned with, over 50 to 100 % of the rows, since
+// how many are kept is known on the device alone (a ragged K takes 256).  Forward with every row kept or as many as named, us, 128 / 192 / 256
+// rows, width 2048, 32000 columns: 16 rows 41 / 47 / 54, 128 48 / 51 / 61, 300 73 / 57 / 64 (128 is chosen, for 150 to 255 of them), 600 of 700 108 / 96 /
+// 108, 1415 of 1665 194 / 181 / 171; width 4096, 128256 columns: 128 rows 212 / 226 / 248, 3400 of 3999 3375 / 2973 / 2878 (squares of 128 45, 49,
+// 78, 108, 204, 234, 3753: nowhere the fastest).
+}  // namespace
+int gemm_lm_height(const GemmArgs& a) {
   if (a.K % 64) return 256;
   int best = 256;
   int64_t least = -1;
@@ -1637,10 +1639,11 @@ int lm_height(const GemmArgs& a) {
   }
   return best;
 }
+namespace {
 template <int LM>
 hipError_t launch_lm(const GemmArgs& a, const LmTarget& t, hipStream_t s) {
   if (a.layout != kNT || !gemm_mfma_supported(a) || a.A2 || (LM == kLmGrad && (a.N % 8 || a.ldc % 8 || ((uintptr_t)a.C & 15)))) return hipErrorInvalidValue;
-  const int BM = lm_height(a);
+  const int BM = gemm_lm_height(a);
   MfmaLmParams p;
   fill_params(p, a, LaunchPlan{BM, 256, kSplitNone, {1, 0, 0}, {0, 0, 0}});
   p.lm = t;

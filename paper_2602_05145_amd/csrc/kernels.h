@@ -77,6 +77,7 @@ struct LmTarget {
   const int32_t* tokens; float2* part; int64_t part_ld; float* label;
   const LmRow* rows; int n0, zero;
 };
+int gemm_lm_height(const GemmArgs& a);   // rows of the tiles that a launch takes (256 columns wide)
 hipError_t launch_gemm_lm_stats(const GemmArgs& a, const LmTarget& t, hipStream_t s);
 hipError_t launch_gemm_lm_grad(const GemmArgs& a, const LmTarget& t, hipStream_t s);
 // fp32, both sizes of the MLP's activations at once.  Forward: gate and up products and h = silu(gate) up in one launch; backward:

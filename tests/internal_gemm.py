@@ -26,6 +26,7 @@ scratch_bytes = _symbol("_ZN4tide25gemm_splitk_scratch_bytesERKNS_8GemmArgsE", C
 scratch_bound = _symbol("_ZN4tide25gemm_splitk_scratch_boundERKNS_8GemmArgsE", C.c_size_t, [C.POINTER(GemmArgs)])
 kernel_name = _symbol("_ZN4tide16gemm_kernel_nameERKNS_8GemmArgsE", C.c_char_p, [C.POINTER(GemmArgs)])
 long_rings = _symbol("_ZN4tide15gemm_long_ringsERKNS_8GemmArgsE", C.c_bool, [C.POINTER(GemmArgs)])
+gemm_lm_height = _symbol("_ZN4tide14gemm_lm_heightERKNS_8GemmArgsE", C.c_int, [C.POINTER(GemmArgs)])
 launch = _symbol("_ZN4tide11launch_gemmERKNS_8GemmArgsEP12ihipStream_t", C.c_int, [C.POINTER(GemmArgs), C.c_void_p])
 
 

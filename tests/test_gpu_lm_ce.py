@@ -4,6 +4,7 @@ import torch
 
 from paper_2602_05145_amd import binding as B
 from tests.gpu_util import stream, sync
+from tests.internal_gemm import NT, args, gemm_lm_height
 from tests.loss_util import CODE, DEV, HALF, STEP, TDT, assert_within, gen, sum_rel
 
 pytestmark = pytest.mark.gpu
@@ -126,6 +127,32 @@ def test_several_pieces(dtype, rows, vocab, d):
     assert off < (2.0 ** -8 if dtype == "bf16" else 1e-5), off
     by_row = (dw.double() - want_dw).norm(dim=1) / (want_dw.norm(dim=1) + 1e-4 * want_dw.norm())
     assert float(by_row.max()) < (2.0 ** -6 if dtype == "bf16" else 1e-4), int(by_row.argmax())   # no row of a piece's edge is wrong
+
+
+HEIGHTS = [(100, 5003, 128, 128), (500, 3000, 64, 128), (1025, 9001, 64, 192), (700, 16000, 128, 192), (2100, 9001, 64, 256), (900, 16000, 128, 256), (200, 3001, 72, 256)]
+
+
+@pytest.mark.parametrize("rows,vocab,d,height", HEIGHTS)
+def test_every_height_of_tiles(rows, vocab, d, height):
+    """Tiles of 128, 192 and 256 rows, and 256 over a width that is no whole number of slabs; every row kept, and a few."""
+    assert gemm_lm_height(args(NT, rows, vocab, d)) == height
+    y, w, tokens, mask = head(rows, vocab, d, "bf16", seed=rows)
+    mask[:] = 1
+    check(y, w, tokens, mask)
+    mask[rows // 3:] = 0
+    check(y, w, tokens, mask)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [7, 8, 9, 1024, 8191, 8192, 8193, 9216, 20481])
+@pytest.mark.parametrize("pattern", ["all", "none", "last", "first", "every third", "not the first thousands"])
+def test_kept_rows_are_found_in_any_number(dtype, rows, pattern):
+    """Up to 8192 rows the blocks count what lies before them by themselves, beyond from counts of 1024 each."""
+    y, w, tokens, mask = head(rows, 64, 8, dtype, seed=rows)
+    i = torch.arange(rows, device=DEV)
+    keep = {"all": i >= 0, "none": i < 0, "last": i == rows - 1, "first": i == 0, "every third": i % 3 == 1, "not the first thousands": i >= rows // 2}[pattern]
+    mask.copy_(keep.to(torch.uint8))
+    check(y, w, tokens, mask)
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
