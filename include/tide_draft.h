@@ -417,7 +417,7 @@ int tide_ce_train(int64_t rows, int32_t vocab, void *z, int64_t ldz, const int32
 
 /* The largest logits of every row, what a served target leaves of its answer for a draft to be trained on (Sec. 3.2: signals
  * are captured while serving; k logits per position are 2 * k numbers where the whole row would be vocab):
- * z [rows, ldz] (DEVICE, dtype TIDE_DTYPE_*, ldz a multiple of 8, >= vocab and <= 2^30, rows 16-byte aligned) is read;
+ * z [rows, ldz] (DEVICE, dtype TIDE_DTYPE_*, ldz a multiple of 8, >= vocab and <= 2^28, rows 16-byte aligned) is read;
  *   ids    DEVICE int32 [rows, k], values DEVICE float [rows, k]: the k largest of columns [0, vocab), the largest first, equal
  *          values (the two zeros too) by ascending column; a NaN counts as larger than every number.  Columns [vocab, ldz) may
  *          hold anything.

@@ -184,16 +184,18 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
   const size_t row = blockIdx.x;
   const T* zr = z + row * (size_t)ldz;
   const float c = scalar(kLog2e / tau);
-  const int last = (V - 1) / 8 * 8;                 // the last chunk: whole in memory, since rows are multiples of eight apart
   if (threadIdx.x < 3) added[threadIdx.x] = 0;
   if (threadIdx.x == 3) { first_any = 0; first_all = ~0u; found_n = 0; }
   lds_barrier();
 
   Raw8Once<T> ring[D][U];                           // the next D rounds
+  // (a buffer's loads take one addition each, and give zeros behind the row)
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(zr), 0, (int)((uint32_t)ldz * (uint32_t)sizeof(T)), 0x00020000);
+  const int lane_at = (int)(threadIdx.x * 8 * sizeof(T));
   auto load = [&](Raw8Once<T> (&raw)[U], int base) {
     if (base < V) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u].load_once(zr, (size_t)min(base + (int)(threadIdx.x + u * NT) * 8, last));
+      for (int u = 0; u < U; ++u) raw[u].load_buffer(rs, lane_at + (base + u * NT * 8) * (int)sizeof(T));
     }
   };
 #pragma unroll
@@ -289,8 +291,8 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
       float v[8];
       columns(cur[u], col, tail, v);
       const float cm = max8(v);
-      const bool pass = col < V && !(cm <= T_v);
-      who[u] = __ballot(pass);
+      who[u] = __ballot(!(cm <= T_v));
+      if (tail) who[u] &= __ballot(col < V);
       top[u] = cm;
       if (who[u] && __any(cm > m)) raise(fast_max(cm));
       float part = 0.f;

@@ -1612,7 +1612,7 @@ hipError_t launch_lm_tiles(MfmaLmParams& p, hipStream_t s) {
   p.tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + 255) / 256;
   const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(512);
-  if constexpr (BM == 256) {
+  if constexpr (BM != 192) {
     if (!whole_slabs(p)) {
       hipLaunchKernelGGL((gemm_mfma_lm_kernel<BM, 256, false, LM>), grid, blk, 0, s, p);
       return hipGetLastError();
@@ -1622,16 +1622,16 @@ hipError_t launch_lm_tiles(MfmaLmParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 // Height of the tiles of the head's logits: the cheapest by the costs that all products are planned with, over 50 to 100 % of the rows, since
-// how many are kept is known on the device alone (a ragged K takes 256).  Forward with every row kept or as many as named, us, 128 / 192 / 256
+// how many are kept is known on the device alone.  Forward with every row kept or as many as named, us, 128 / 192 / 256
 // rows, width 2048, 32000 columns: 16 rows 41 / 47 / 54, 128 48 / 51 / 61, 300 73 / 57 / 64 (128 is chosen, for 150 to 255 of them), 600 of 700 108 / 96 /
 // 108, 1415 of 1665 194 / 181 / 171; width 4096, 128256 columns: 128 rows 212 / 226 / 248, 3400 of 3999 3375 / 2973 / 2878 (squares of 128 45, 49,
 // 78, 108, 204, 234, 3753: nowhere the fastest).
 }  // namespace
 int gemm_lm_height(const GemmArgs& a) {
-  if (a.K % 64) return 256;
   int best = 256;
   int64_t least = -1;
   for (const int BM : {256, 192, 128}) {
+    if (BM == 192 && a.K % 64) continue;   // (only with whole slabs)
     int64_t t = 0;
     for (int share = 10; share <= 20; ++share)
       t += launch_time(a, LaunchPlan{BM, 256, kSplitNone, {1, 0, 0}, {0, 0, 0}}, std::max<int64_t>(1, a.M * share / 20));

@@ -64,6 +64,10 @@ __device__ __forceinline__ Online online_block(const Online& o, float c, Online*
 }
 
 template <typename T> struct Raw8Once : Raw8<T> {   // loads past the caches: nothing is read again
+  __device__ __forceinline__ void load_buffer(__amdgpu_buffer_rsrc_t rs, int at) {   // from byte `at`
+    this->a = __builtin_bit_cast(decltype(this->a), __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 2));
+    if constexpr (sizeof(T) == 4) this->b = __builtin_bit_cast(decltype(this->b), __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16, 0, 2));
+  }
   __device__ __forceinline__ void load_once(const T* p, size_t i) {
     typedef unsigned u32x4_nt __attribute__((ext_vector_type(4)));
     const u32x4_nt* q = reinterpret_cast<const u32x4_nt*>(p + i);

@@ -1201,7 +1201,7 @@ int tide_ce_train(int64_t rows, int32_t vocab, void* z, int64_t ldz, const int32
 }
 
 static bool logits_ok(int64_t rows, int32_t vocab, const void* z, int64_t ldz, float temperature, int dtype) {
-  if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || ldz < vocab || ldz % 8 || ldz > (1 << 30)) { fail(TIDE_ERR_CONFIG, "bad logit block shape"); return false; }
+  if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || ldz < vocab || ldz % 8 || ldz > (1 << 28)) { fail(TIDE_ERR_CONFIG, "bad logit block shape"); return false; }
   if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
   if (!(temperature >= 1e-6f && temperature <= 1e6f)) { fail(TIDE_ERR_CONFIG, "temperature must be in [1e-6, 1e6]"); return false; }
   if (((uintptr_t)z) & 15) { fail(TIDE_ERR_CONFIG, "z must be 16-byte aligned"); return false; }

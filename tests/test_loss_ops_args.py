@@ -28,7 +28,7 @@ def lm_bwd(rows=4, vocab=100, d=64, y=P, w=P, tokens=P, mask=P, lse=P, weights=N
     return B.tide_lm_ce_bwd(rows, vocab, d, y, w, tokens, mask, lse, weights, scale, dy, dw, dw_dtype, dtype, ws, n, None, check=False)
 
 
-BAD_LOGITS = [dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=-3), dict(ldz=96), dict(ldz=108), dict(ldz=(1 << 30) + 8), dict(z=P + 8), dict(dtype=2), dict(dtype=-1),
+BAD_LOGITS = [dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=-3), dict(ldz=96), dict(ldz=108), dict(ldz=(1 << 28) + 8), dict(z=P + 8), dict(dtype=2), dict(dtype=-1),
               dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=1e-7), dict(temperature=2e6), dict(temperature=float("nan")), dict(temperature=float("inf")), dict(k=0), dict(k=-1), dict(k=129)]
 
 
