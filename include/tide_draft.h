@@ -423,11 +423,12 @@ int tide_ce_train(int64_t rows, int32_t vocab, void *z, int64_t ldz, const int32
  *          hold anything.
  *   lse    DEVICE float [rows] or NULL: the log-sum-exp of z / temperature (-inf for a row of -inf, +inf for one that holds +inf,
  *          NaN for one that holds NaN and no +inf)
- * 1 <= k <= min(vocab, 128), temperature in [1e-6, 1e6]; rows may be 0 (the arrays may be NULL then).  Enqueues one kernel and nothing else. */
+ * 1 <= k <= min(vocab, 128), temperature in [1e-6, 1e6], rows < 2^22; rows may be 0 (the arrays may be NULL then).  Enqueues one kernel
+ * and nothing else. */
 int tide_topk_logits(int64_t rows, int32_t vocab, const void *z, int64_t ldz, int32_t k, float temperature,
                      int32_t *ids, float *values, float *lse, int dtype, void *stream);
 
-/* Distillation of a block of student logits z [rows, ldz] (as in tide_ce_train) from a teacher's top logits.  Of row r, over its
+/* Distillation of a block of student logits z [rows, ldz] (as in tide_topk_logits) from a teacher's top logits.  Of row r, over its
  * entries j with 0 <= teacher_ids[r, j] < vocab (others are ignored, so that a row may have fewer than k), with
  * a_j = teacher_logits[r, j] / temperature:
  *     p_j  = exp(a_j - L),  L = log-sum-exp of these a_j, or teacher_lse[r] if teacher_lse is given (the log-sum-exp of the
@@ -441,8 +442,8 @@ int tide_topk_logits(int64_t rows, int32_t vocab, const void *z, int64_t ldz, in
  *   teacher_ids DEVICE int32 [rows, k], teacher_logits DEVICE float [rows, k], teacher_lse DEVICE float [rows] or NULL
  *   mask, lse, loss_rows  DEVICE [rows]
  *   dz   DEVICE, layout and dtype of z: z itself (in place) or an array that does not overlap it
- * tide_distill_eval gives lse and loss_rows alone and leaves z as it is.  1 <= k <= 128, temperature in [1e-6, 1e6]; rows may be 0 (the arrays
- * may be NULL then).
+ * tide_distill_eval gives lse and loss_rows alone and leaves z as it is.  1 <= k <= 128, temperature in [1e-6, 1e6], rows < 2^22; rows
+ * may be 0 (the arrays may be NULL then).
  * Each call enqueues one kernel and nothing else. */
 int tide_distill_eval(int64_t rows, int32_t vocab, const void *z, int64_t ldz, int32_t k, const int32_t *teacher_ids,
                       const float *teacher_logits, const float *teacher_lse, float temperature, const uint8_t *mask,
@@ -466,7 +467,7 @@ int tide_distill_train(int64_t rows, int32_t vocab, const void *z, void *dz, int
  *   workspace    DEVICE, 256-byte aligned, of at least tide_lm_ce_workspace_bytes(rows, vocab, d, dtype) bytes (0 = sizes the
  *                calls refuse); the same size serves both calls, nothing in it has to survive between them, and calls that overlap
  *                need one each.  It never falls as rows grow.
- * rows in [1, 2^22], vocab and d in [1, 2^21); bf16: d a multiple of 8, vocab >= 8; y, w, dy and dw 16-byte aligned.
+ * rows in [1, 2^21], vocab and d in [1, 2^21), rows * vocab <= 2^37; no output overlaps an input; bf16: d a multiple of 8, vocab >= 8; y, w, dy and dw 16-byte aligned.
  * dtype TIDE_DTYPE_BF16: logits and sums are fp32; dz is rounded to bf16 (it is an operand of the two products), and dy and a
  * bf16 dw once from their fp32 sums.  Enqueues kernels on `stream` and nothing else. */
 size_t tide_lm_ce_workspace_bytes(int64_t rows, int32_t vocab, int64_t d, int dtype);

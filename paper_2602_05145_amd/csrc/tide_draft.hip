@@ -1201,7 +1201,8 @@ int tide_ce_train(int64_t rows, int32_t vocab, void* z, int64_t ldz, const int32
 }
 
 static bool logits_ok(int64_t rows, int32_t vocab, const void* z, int64_t ldz, float temperature, int dtype) {
-  if (rows < 0 || rows > 0x7fffffff || vocab <= 0 || ldz < vocab || ldz % 8 || ldz > (1 << 28)) { fail(TIDE_ERR_CONFIG, "bad logit block shape"); return false; }
+  // (a block of up to 1024 threads per row, and a launch holds fewer than 2^32)
+  if (rows < 0 || rows >= (1 << 22) || vocab <= 0 || ldz < vocab || ldz % 8 || ldz > (1 << 28)) { fail(TIDE_ERR_CONFIG, "bad logit block shape"); return false; }
   if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
   if (!(temperature >= 1e-6f && temperature <= 1e6f)) { fail(TIDE_ERR_CONFIG, "temperature must be in [1e-6, 1e6]"); return false; }
   if (((uintptr_t)z) & 15) { fail(TIDE_ERR_CONFIG, "z must be 16-byte aligned"); return false; }
@@ -1242,10 +1243,12 @@ int tide_distill_train(int64_t rows, int32_t vocab, const void* z, void* dz, int
 
 static bool lm_ce_sizes_ok(int64_t rows, int32_t vocab, int64_t d, int dtype) {
   if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
-  if (rows < 1 || rows > ((int64_t)1 << 22) || vocab < 1 || vocab >= (1 << 21) || d < 1 || d >= (1 << 21)) {
-    fail(TIDE_ERR_CONFIG, "rows must be in [1, 2^22], vocab and d in [1, 2^21)");
+  if (rows < 1 || rows > ((int64_t)1 << 21) || vocab < 1 || vocab >= (1 << 21) || d < 1 || d >= (1 << 21)) {
+    fail(TIDE_ERR_CONFIG, "rows must be in [1, 2^21], vocab and d in [1, 2^21)");
     return false;
   }
+  // (blocks of 512 threads for 128 x 256 logits or more, and a launch holds fewer than 2^32)
+  if (rows * vocab > ((int64_t)1 << 37)) { fail(TIDE_ERR_CONFIG, "rows * vocab must be at most 2^37"); return false; }
   if (dtype == TIDE_DTYPE_BF16 && (d % 8 || vocab < 8)) { fail(TIDE_ERR_CONFIG, "bf16: d must be a multiple of 8, and vocab at least 8"); return false; }
   return true;
 }

@@ -86,6 +86,15 @@ def test_lm_ce_refuses_bad_outputs_and_workspaces():
         assert call(ws=P + 128) == B.TIDE_ERR_WORKSPACE
 
 
+def test_more_rows_than_a_launch_holds_are_refused():
+    for rows in (1 << 22, 1 << 23, 1 << 25):
+        assert topk(rows=rows) == distill(True, rows=rows) == distill(False, rows=rows) == B.TIDE_ERR_CONFIG
+    for rows, vocab in (((1 << 21) + 1, 8), (1 << 22, 8), (1 << 21, (1 << 16) + 8), (1 << 21, 128256), ((1 << 37) // 128256 + 1, 128256)):
+        assert lm_fwd(rows=rows, vocab=vocab) == lm_bwd(rows=rows, vocab=vocab) == B.TIDE_ERR_CONFIG
+        assert B.tide_lm_ce_workspace_bytes(rows, vocab, 64, BF16) == 0
+    assert B.tide_lm_ce_workspace_bytes(1 << 20, 128256, 64, BF16) > 0
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("vocab", [8, 1000, 32001, 128256])
 def test_lm_ce_workspace_never_falls_as_rows_grow(dtype, vocab):
