@@ -738,7 +738,18 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     buf[i] = chunk_grad(buf[i], pw.slope, sh, g.scale);
     store(buf[i], c0, i * STEP * (int)sizeof(T));
   }
-  for (int i = 0; i < n_lds; ++i) store(chunk_grad(mine[i * NT], pw.slope, sh, g.scale), c0 + (NREG + i) * STEP, 0);
+  for (int i = 0; i < n_lds; ++i) {
+    const int col = c0 + (NREG + i) * STEP, nv = V - col;
+    u32x4_t v = chunk_grad(mine[i * NT], pw.slope, sh, g.scale);
+    if (nv < E) {   // padded columns are 0 also where the row's sums are not numbers
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (sizeof(T) == 2) v[k] = 2 * k + 1 < nv ? v[k] : 2 * k < nv ? v[k] & 0xFFFFu : 0u;
+        else v[k] = k < nv ? v[k] : 0u;
+      }
+    }
+    store(v, col, 0);
+  }
   teacher_store<T, NT, E>(te, a.k, dr);
 }
 

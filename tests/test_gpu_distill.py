@@ -140,6 +140,20 @@ def test_rows_without_loss_may_hold_anything(dtype, vocab):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab,extra", [(5, 16), (700, 8), (4099, 24), (33001, 8), (200001, 8)])
+def test_padded_columns_are_zero_in_rows_without_a_number(dtype, vocab, extra):
+    z = logits(4, vocab, padded(vocab, extra), dtype, 9)
+    z[0, :vocab] = -torch.inf          # no softmax
+    z[1, vocab // 2] = float("nan")
+    z[2, vocab - 1] = torch.inf
+    ids, t = teacher(4, vocab, 4, 9)
+    for in_place in (False, True):
+        _, _, dz = call(z, vocab, ids, t, None, 1.0, torch.ones(4, device=DEV, dtype=torch.uint8), in_place=in_place)
+        assert bool((dz[:, vocab:] == 0).all())
+        assert bool(dz[:2, :vocab].isnan().all()) and bool(dz[3, :vocab].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_masked_columns_and_confident_rows(dtype):
     """-inf and the type's lowest value as masks of columns; a teacher entry on a column that the student excludes costs +inf."""
     vocab, k = 5000, 6
