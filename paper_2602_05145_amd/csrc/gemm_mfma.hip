@@ -626,7 +626,8 @@ __device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamPara
   // ---- epilogues of logits that are not kept.  z = the accumulators; token(row) - first column of the wave = the label's place in it. ----
   // Forward: of every row, the maximum and the sum of exponentials over this tile's columns (a row of a wave's 64 columns lies in four
   // lanes of 16 values; the waves side by side meet in LDS), and the label's logit from the one tile that holds it.
-  // 256 x 256: 128 exponentials a lane, about 4 us behind 85 us of products at K = 4096.
+  // 128 exponentials a lane of a 256 x 256 tile in place of its 128 KB of stores: [27853, 128256], width 4096, 22.0 ms with the rows' copy and the
+  // join, the product that writes its logits 22.1.
   [[maybe_unused]] auto lm_stats = [&](bf16_t* lds) {
     if constexpr (LM == kLmStats) {
       constexpr float LOG2E = 1.4426950408889634f;
