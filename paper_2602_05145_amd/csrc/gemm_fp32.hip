@@ -15,6 +15,7 @@
 // Contraction order.  A 32x32x2 instruction takes k values {a, b} from the lower and the upper half of the wave
 // (16x16x4: four, from its quarters).  The kernels feed it {8 s + i, 8 s + 4 + i} for i = 0..3: a lane's four values of a group of 8 k are consecutive,
 // one 16-byte read of an operand whose contraction index is contiguous.
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -40,6 +41,8 @@ struct Fp32GemmParams {
   // SwiGLU's backward behind the product of dh (EXT instantiations): gt and u share C's layout and become dgate and dup
   float *gt, *u;
 };
+// one of several sums over K: blocks of z take k_part of it each, and leave their sum `stride` elements behind the one before
+struct Fp32PartsParams : Fp32GemmParams { int k_part; int64_t stride; };
 
 // sizes that are only known on the device (block-uniform)
 __device__ __forceinline__ void device_sizes(Fp32GemmParams& p) {
@@ -83,8 +86,8 @@ __device__ __forceinline__ void store_c(const Fp32GemmParams& p, float alpha, in
 }  // namespace
 
 // ---- tiles of 128 x 128 (T = 2) or 64 x 64 (T = 1): four waves, each T x T instruction tiles of 32 x 32 ----
-template <int T, bool AKM, bool BKM, bool VEC>
-__global__ __launch_bounds__(256, 2) void gemm_fp32_tile_kernel(Fp32GemmParams p) {
+template <int T, bool AKM, bool BKM, bool VEC, bool PARTS = false>
+__global__ __launch_bounds__(256, 2) void gemm_fp32_tile_kernel(std::conditional_t<PARTS, Fp32PartsParams, Fp32GemmParams> p) {
   constexpr int BT = 64 * T, BK = 32;
   // K-major operand: [row][k], pitch 36: the 16 rows of a 16-byte read start 4 banks * 9 apart, i.e. on 16 different
   // bank groups.  Row-major operand: [k][row], pitch BT + 8: the two k-rows of a read, 4 apart, lie on opposite
@@ -95,6 +98,13 @@ __global__ __launch_bounds__(256, 2) void gemm_fp32_tile_kernel(Fp32GemmParams p
   __shared__ __attribute__((aligned(16))) float sA[2][ASZ];
   __shared__ __attribute__((aligned(16))) float sB[2][BSZ];
   device_sizes(p);
+  if constexpr (PARTS) {
+    const int64_t k0 = (int64_t)blockIdx.z * p.k_part;
+    p.A += AKM ? k0 : k0 * p.lda;
+    p.B += BKM ? k0 : k0 * p.ldb;
+    p.K = (int)max((int64_t)0, min((int64_t)p.k_part, p.K - k0));
+    p.C += (int64_t)blockIdx.z * p.stride;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lr = lane & 31, g = lane >> 5;
   const int m0 = blockIdx.y * BT, n0 = blockIdx.x * BT;
@@ -456,6 +466,30 @@ hipError_t launch_gemm_fp32(const GemmArgs& a, hipStream_t s) {
     case kTN: return launch_fp32_vec<false, false>(p, vec, s);
     default: return hipErrorInvalidValue;
   }
+}
+
+// A product with a long contraction and few tiles (dy of a loss over a vocabulary): tiles of 64 x 64, the contraction in as many parts as make
+// kFp32PartsTiles of them, each of 128 or more.  Product, its consumer and what else a head's backward pass launches for dy, us, one launch / 8 / 16 /
+// 32 parts: 128 x 256 x 4096 34.7 / 37.9 / 31.5 / 29.9, 32 x 2048 x 32000 234 / 269 / 221 / 203, 100 x 2048 x 32000 481 / 392 / 352 / 357; 1 / 4 /
+// 8 parts: 400 x 2048 x 32000 1824 / 1268 / 1226; 1 / 2 / 3: 2500 x 2048 x 32000 8325 / 6169 / 6089, 4000 x 2048 x 32000 9791 / 9789 / 9693.
+int gemm_fp32_parts(int64_t M, int64_t N, int64_t K) {
+  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
+  return (int)std::max<int64_t>(1, std::min({(int64_t)kMaxFp32Parts, (kFp32PartsTiles + tiles - 1) / tiles, K / 128}));
+}
+hipError_t launch_gemm_fp32_parts(const GemmArgs& a, int parts, int64_t stride, hipStream_t s) {
+  if (parts == 1) return launch_gemm(a, s);
+  Fp32PartsParams p;
+  bool vec;
+  if (a.layout != kNN || a.in_dtype != kF32 || a.out_dtype != kF32 || a.M <= 0 || a.N <= 0 || a.residual || a.A2 || a.k_dev || !fp32_params(a, p, vec) ||
+      (a.M + 63) / 64 > 65535) return hipErrorInvalidValue;
+  p.k_part = (int)((a.K + parts - 1) / parts + 31) / 32 * 32;
+  p.stride = stride;
+  ProfScope ps("gemm_fp32_parts", 2.0 * a.M * a.N * (double)a.K, 4.0 * (a.K * (a.M + (double)a.N) + parts * a.M * (double)a.N), s);
+  if (a.m_dev) prof_dynamic(a.m_dev, a.m_off, a.M);
+  const dim3 grid((unsigned)((a.N + 63) / 64), (unsigned)((a.M + 63) / 64), (unsigned)parts);
+  if (vec) hipLaunchKernelGGL((gemm_fp32_tile_kernel<1, true, false, true, true>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((gemm_fp32_tile_kernel<1, true, false, false, true>), grid, dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 // n independent products, one launch when all of them are fp32, of one layout and of the size that the split over four

@@ -68,6 +68,12 @@ constexpr int kMaxGemmGroup = 6;
 bool gemm_adam_group_pays(int64_t rows);
 hipError_t launch_gemm_adam_group(const GemmArgs* a, const AdamTarget* t, int n, hipStream_t s);
 hipError_t launch_gemm_group(const GemmArgs* a, int n, hipStream_t s);  // independent products, in one launch where small
+// fp32, NN: a product as up to kMaxFp32Parts sums over K, `stride` elements apart (each with alpha, and on top of what is there where it accumulates),
+// for a consumer that adds them up.  gemm_fp32_parts: how many pay; with more than one they hold at most
+// 2 kFp32PartsTiles 64^2 elements together.
+constexpr int kMaxFp32Parts = 32, kFp32PartsTiles = 1536;
+int gemm_fp32_parts(int64_t M, int64_t N, int64_t K);
+hipError_t launch_gemm_fp32_parts(const GemmArgs& a, int parts, int64_t stride, hipStream_t s);
 // The LM head's logits z = y W^T (NT, bf16) that are not kept.  Forward: part[t * part_ld + row] = the maximum of z and the sum of
 // exp(z - that) over the t-th kLmColumns columns, label[row] = z[row, tokens[row]] where the launch's columns hold it.
 // Backward: C = weight (exp(z - lse) - [column == token]) in bf16, for columns n0 + c of the vocabulary; the first `zero` columns get 0.

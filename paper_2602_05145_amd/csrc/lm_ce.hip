@@ -81,7 +81,8 @@ LmCePlan make_plan(int64_t rows, int64_t V, int64_t d, int dtype) {
   p.y_c = take(T * d * es);
   p.z = take(std::max((size_t)piece_elems(rows, V, dtype) * es, dtype == kBF16 ? T * (size_t)((V + kLmColumns - 1) / kLmColumns) * sizeof(float2) : 0));
   p.acc = pc.count > 1 && dtype == kBF16 ? take(T * d * 4) : 0;
-  p.dy_c = take(T * d * es);
+  // fp32: as many sums of it as the product leaves (see gemm_fp32_parts), within a bound that does not fall as rows grow
+  p.dy_c = take(dtype == kF32 ? std::max(T * d, std::min(kMaxFp32Parts * T * d, (size_t)2 * kFp32PartsTiles * 4096)) * es : T * d * es);
   if (dtype == kF32 || pc.count == 1) p.acc = p.dy_c;
   p.split_bytes = 0;
   if (dtype == kBF16) {
@@ -264,9 +265,9 @@ __global__ __launch_bounds__(256) void lm_grad_kernel(float* z, int64_t ldz, int
   }
 }
 
-// compact rows back to their places, zeros elsewhere
+// compact rows back to their places, zeros elsewhere.  A row is the sum of `parts`, `stride` elements apart.
 template <typename TI, typename TO>
-__global__ __launch_bounds__(256) void lm_scatter_kernel(const TI* __restrict__ src, TO* __restrict__ dst, int d, const int32_t* __restrict__ row_pos) {
+__global__ __launch_bounds__(256) void lm_scatter_kernel(const TI* __restrict__ src, TO* __restrict__ dst, int d, const int32_t* __restrict__ row_pos, int parts, int64_t stride) {
   const size_t t = blockIdx.x;
   const int i = row_pos[t];
   TO* b = dst + t * (size_t)d;
@@ -275,10 +276,23 @@ __global__ __launch_bounds__(256) void lm_scatter_kernel(const TI* __restrict__ 
     for (int c = threadIdx.x * 8; c < d; c += 256 * 8) {
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (i >= 0) ld8(a, c, v);
+      if constexpr (sizeof(TI) == 4 && sizeof(TO) == 4) {
+#pragma unroll 4
+        for (int q = 1; q < parts && i >= 0; ++q) {
+          float x[8];
+          ld8(a + q * stride, c, x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+      }
       st8(b, c, v);
     }
   } else {
-    for (int c = threadIdx.x; c < d; c += 256) stf(b, c, i < 0 ? 0.f : ldf(a, c));
+    for (int c = threadIdx.x; c < d; c += 256) {
+      float v = i < 0 ? 0.f : ldf(a, c);
+      for (int q = 1; q < parts && i >= 0; ++q) v += ldf(a + q * stride, c);
+      stf(b, c, v);
+    }
   }
 }
 
@@ -362,6 +376,8 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
   const int64_t ld = piece_ld(c.pc);
   const bool bf16 = a.dtype == kBF16, to_acc = bf16 && c.pc.count > 1;
   const LmRow* rows = c.at<LmRow>(c.p.rows_c);
+  const int parts = bf16 ? 1 : gemm_fp32_parts(a.rows, a.d, c.pc.width);
+  const int64_t part_stride = a.rows * a.d;
   for (int i = 0; i < c.pc.count; ++i) {
     const Piece q = piece_at(c.pc, i);
     if (bf16) {
@@ -377,7 +393,8 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
     g.m_dev = c.cnt();
     g.alpha = a.scale;
     g.accumulate = i > 0;
-    LM_TRY(c.with_scratch(g));
+    if (bf16) LM_TRY(c.with_scratch(g));
+    else LM_TRY(launch_gemm_fp32_parts(g, parts, part_stride, s));
     if (a.dw) {
       GemmArgs w = product(kTN, q.n, a.d, a.rows, c.ws + c.p.z, ld, c.ws + c.p.y_c, a.d, (char*)a.dw + (size_t)q.n0 * a.d * dtype_size(a.dw_dtype), a.d,
                            a.dtype, a.dw_dtype);
@@ -389,9 +406,9 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
   ProfScope ps("lm_ce_scatter", 0, (double)a.rows * a.d * (dtype_size(a.dtype) + (to_acc ? 4.0 : dtype_size(a.dtype))), s);
   const dim3 grid((unsigned)a.rows), blk(256);
   const int32_t* row_pos = c.at<int32_t>(c.p.row_pos);
-  if (to_acc) hipLaunchKernelGGL((lm_scatter_kernel<float, bf16_t>), grid, blk, 0, s, c.at<float>(c.p.acc), (bf16_t*)a.dy, (int)a.d, row_pos);
-  else if (bf16) hipLaunchKernelGGL((lm_scatter_kernel<bf16_t, bf16_t>), grid, blk, 0, s, c.at<bf16_t>(c.p.acc), (bf16_t*)a.dy, (int)a.d, row_pos);
-  else hipLaunchKernelGGL((lm_scatter_kernel<float, float>), grid, blk, 0, s, c.at<float>(c.p.acc), (float*)a.dy, (int)a.d, row_pos);
+  if (to_acc) hipLaunchKernelGGL((lm_scatter_kernel<float, bf16_t>), grid, blk, 0, s, c.at<float>(c.p.acc), (bf16_t*)a.dy, (int)a.d, row_pos, parts, part_stride);
+  else if (bf16) hipLaunchKernelGGL((lm_scatter_kernel<bf16_t, bf16_t>), grid, blk, 0, s, c.at<bf16_t>(c.p.acc), (bf16_t*)a.dy, (int)a.d, row_pos, parts, part_stride);
+  else hipLaunchKernelGGL((lm_scatter_kernel<float, float>), grid, blk, 0, s, c.at<float>(c.p.acc), (float*)a.dy, (int)a.d, row_pos, parts, part_stride);
   return hipGetLastError();
 }
 

@@ -143,6 +143,12 @@ def test_every_height_of_tiles(rows, vocab, d, height):
     check(y, w, tokens, mask)
 
 
+# the gradient of the hidden states as 32 sums over the vocabulary, of which the last are empty; 5; 2; and one of 4100 rows
+@pytest.mark.parametrize("rows,vocab,d", [(1, 4097, 264), (115, 4096, 256), (70, 16389, 33), (65, 4099, 2056), (333, 700, 64), (130, 300, 72), (4100, 300, 1536)])
+def test_fp32_sums_over_parts_of_the_vocabulary(rows, vocab, d):
+    check(*head(rows, vocab, d, "fp32", seed=vocab), scale=0.25)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows", [7, 8, 9, 1024, 8191, 8192, 8193, 9216, 20481])
 @pytest.mark.parametrize("pattern", ["all", "none", "last", "first", "every third", "not the first thousands"])
