@@ -349,7 +349,8 @@ __global__ __launch_bounds__(256) void gemm_fp32_group_kernel(Fp32Group g) {
 
 namespace {
 
-// Which kernel.  The large tile when it gives every CU one; the small one, or the 32-row tile of the split over waves,
+// Which kernel.  The large tile when it gives every CU one and has more than 64 rows and columns to fill (NT 16 x 128256 x 2048 595 us with it, 325
+// with the small one; 65 rows 602 / 598); the small one, or the 32-row tile of the split over waves,
 // when it gives three CUs in four one (300 x 2048 x 2048: 54 us with 160 tiles of 64 refused, 79 us with them; 512 x 256 x
 // 4096: 30 us with 128 tiles of 32 refused, 40 with them); else tiles of 16.  Sixteen waves from K = 1024 on
 // (TN 688 x 256 x 512: 8 us with four, 55 with sixteen, whose blocks then have two loads each; NN 128 x 256 x 4096 needs
@@ -375,7 +376,7 @@ hipError_t launch_fp32_layout(const Fp32GemmParams& p, hipStream_t s) {
   auto tiles = [&](int64_t e) { return ((p.M + e - 1) / e) * ((p.N + e - 1) / e); };
   auto grid = [&](int e) { return dim3((unsigned)((p.N + e - 1) / e), (unsigned)((p.M + e - 1) / e)); };
   if constexpr (!EXT) {   // (see gemm_swiglu_supported)
-    if (tiles(128) >= kBigTiles) {
+    if (tiles(128) >= kBigTiles && p.M > 64 && p.N > 64) {
       hipLaunchKernelGGL((gemm_fp32_tile_kernel<2, AKM, BKM, VEC>), grid(128), dim3(256), 0, s, p);
       return hipGetLastError();
     }
