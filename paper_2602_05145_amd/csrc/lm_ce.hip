@@ -217,34 +217,50 @@ __global__ __launch_bounds__(256) void lm_stats_kernel(const float* __restrict__
   }
 }
 
-// bf16: a row's statistics of all tiles as one.  Sixteen rows per block (their pairs lie side by side), sixteen threads each.
-__global__ __launch_bounds__(256) void lm_join_kernel(const float2* __restrict__ part, int64_t part_ld, int tiles, const float* __restrict__ label,
-                                                      const int32_t* __restrict__ kept_idx, const int* __restrict__ cnt,
-                                                      float* __restrict__ lse, float* __restrict__ loss_rows) {
+// bf16: a row's statistics of all tiles as one.  Sixteen rows per block (their pairs lie side by side), 64 threads each, four pairs at a time.
+__global__ __launch_bounds__(1024) void lm_join_kernel(const float2* __restrict__ part, int64_t part_ld, int tiles, const float* __restrict__ label,
+                                                       const int32_t* __restrict__ kept_idx, const int* __restrict__ cnt,
+                                                       float* __restrict__ lse, float* __restrict__ loss_rows) {
+  constexpr int U = 4, BY = 64;
   __shared__ float2 st[16][17];
   const int r = threadIdx.x & 15, by = threadIdx.x >> 4;
   const int64_t i = (int64_t)blockIdx.x * 16 + r;
   const int n = *cnt;
+  if ((int64_t)blockIdx.x * 16 >= n) return;   // whole block
   float2 o = make_float2(-INFINITY, 0.f);
-  auto join = [](float2 a, float2 b) {
+  auto scaled = [](float2 x, float m) { return m > -INFINITY ? x.y * __builtin_amdgcn_exp2f((x.x - m) * kLog2e) : x.y; };   // (below any number: 0, or NaN)
+  auto join = [&](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x);
-    if (m > -INFINITY) a.y = a.y * expf(a.x - m) + b.y * expf(b.x - m);
-    else a.y += b.y;                          // 0, or NaN
-    a.x = m;
-    return a;
+    return make_float2(m, scaled(a, m) + scaled(b, m));
   };
   if (i < n) {
-#pragma unroll 4
-    for (int t = by; t < tiles; t += 16) o = join(o, part[(size_t)t * part_ld + i]);
+    for (int t = by; t < tiles; t += U * BY) {
+      float2 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = t + u * BY < tiles ? part[(size_t)(t + u * BY) * part_ld + i] : make_float2(-INFINITY, 0.f);
+      float m = o.x;
+#pragma unroll
+      for (int u = 0; u < U; ++u) m = fmaxf(m, x[u].x);
+      o.y = scaled(o, m);
+#pragma unroll
+      for (int u = 0; u < U; ++u) o.y += scaled(x[u], m);
+      o.x = m;
+    }
   }
-  st[by][r] = o;
+#pragma unroll
+  for (int d = 16; d < 64; d *= 2) o = join(o, make_float2(__shfl_xor(o.x, d, 64), __shfl_xor(o.y, d, 64)));
+  if ((threadIdx.x & 63) < 16) st[threadIdx.x >> 6][r] = o;
   __syncthreads();
-  if (by == 0 && i < n) {
-    for (int k = 1; k < 16; ++k) o = join(o, st[k][r]);
-    const float log_s = logf(o.y);
+  if (threadIdx.x < 16 && i < n) {
+    float m = -INFINITY, s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m = fmaxf(m, st[k][r].x);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s += scaled(st[k][r], m);
+    const float log_s = logf(s);
     const int at = kept_idx[i];
-    lse[at] = o.x + log_s;
-    loss_rows[at] = log_s + (o.x - label[i]);
+    lse[at] = m + log_s;
+    loss_rows[at] = log_s + (m - label[i]);
   }
 }
 
@@ -353,7 +369,7 @@ hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s) {
     LM_TRY(launch_gemm_lm_stats(g, t, s));
     ProfScope ps("lm_ce_join", 0, 8.0 * (double)a.rows * tiles, s);
     prof_dynamic(c.cnt(), 0, a.rows);
-    hipLaunchKernelGGL(lm_join_kernel, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), 0, s, t.part, t.part_ld, tiles, label,
+    hipLaunchKernelGGL(lm_join_kernel, dim3((unsigned)((a.rows + 15) / 16)), dim3(1024), 0, s, t.part, t.part_ld, tiles, label,
                        c.at<int32_t>(c.p.kept_idx), c.cnt(), a.lse, a.loss_rows);
     return hipGetLastError();
   }
