@@ -125,7 +125,8 @@ __global__ __launch_bounds__(256) void lm_count_kernel(const int32_t* __restrict
 }
 
 // The dense array of the kept rows, in order, with everything that a call needs of each: its hidden state, label, place in the batch, and
-// either a fresh RowState (fp32's forward) or its LmRow (backward).  Eight rows per block, two per wave.  The rows kept before a
+// either a fresh RowState (fp32's forward) or its LmRow (backward).  Four rows per block, one per wave (eight: 90 x 4096 15.7 us, 3400 x 4096 22.9,
+// 27853 x 4096 87.7; four: 11.4, 17.7, 83.0).  The rows kept before a
 // block's are counted by the block itself up to kDirectRows (at most 32 rows per thread), beyond from the counts of
 // kCountRows each: one launch (of 5 us next to nothing in it) instead of three, or two.
 enum : int { kBeginForward = 0, kBeginForwardFp32 = 1, kBeginBackward = 2 };
@@ -139,7 +140,7 @@ struct LmBegin {
 };
 template <typename T>
 __global__ __launch_bounds__(256) void lm_begin_kernel(LmBegin a) {
-  constexpr int ROWS = 8;
+  constexpr int ROWS = 4;
   __shared__ int red[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t t0 = (int64_t)blockIdx.x * ROWS;
@@ -155,39 +156,36 @@ __global__ __launch_bounds__(256) void lm_begin_kernel(LmBegin a) {
   const bool mine = lane < ROWS && t0 + lane < a.T && kept(a.tokens, a.mask, t0 + lane, a.V);
   const uint32_t keep = (uint32_t)__ballot(mine);
   if (t0 + ROWS >= a.T && threadIdx.x == 0) *a.cnt = before + __popc(keep);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = wave * 2 + h;
-    const int64_t t = t0 + r;
-    if (t >= a.T) return;
-    if (!((keep >> r) & 1)) {
-      if (lane == 0) {
-        a.row_pos[t] = -1;
-        if (a.mode != kBeginBackward) a.lse[t] = a.loss_rows[t] = 0.f;
-      }
-      continue;
-    }
-    const int pos = before + __popc(keep & ((1u << r) - 1));
+  const int r = wave;
+  const int64_t t = t0 + r;
+  if (t >= a.T) return;
+  if (!((keep >> r) & 1)) {
     if (lane == 0) {
-      const int token = a.tokens[t];
-      a.row_pos[t] = pos;
-      a.kept_idx[pos] = (int32_t)t;
-      a.tokens_c[pos] = token;
-      if (a.mode == kBeginBackward) reinterpret_cast<LmRow*>(a.rows_c)[pos] = LmRow{-a.lse[t] * 1.4426950408889634f, a.weights ? a.weights[t] : 1.f, token, a.lse[t]};
-      else if (a.mode == kBeginForwardFp32) reinterpret_cast<RowState*>(a.rows_c)[pos] = RowState{-INFINITY, 0.f, 0.f};
+      a.row_pos[t] = -1;
+      if (a.mode != kBeginBackward) a.lse[t] = a.loss_rows[t] = 0.f;
     }
-    const T* src = (const T*)a.y + (size_t)t * a.d;
-    T* dst = (T*)a.y_c + (size_t)pos * a.d;
-    if (a.d % 8 == 0) {
-#pragma unroll 4
-      for (int c = lane * 8; c < a.d; c += 64 * 8) {
-        float v[8];
-        ld8(src, c, v);
-        st8(dst, c, v);
-      }
-    } else {
-      for (int c = lane; c < a.d; c += 64) dst[c] = src[c];
+    return;
+  }
+  const int pos = before + __popc(keep & ((1u << r) - 1));
+  if (lane == 0) {
+    const int token = a.tokens[t];
+    a.row_pos[t] = pos;
+    a.kept_idx[pos] = (int32_t)t;
+    a.tokens_c[pos] = token;
+    if (a.mode == kBeginBackward) reinterpret_cast<LmRow*>(a.rows_c)[pos] = LmRow{-a.lse[t] * 1.4426950408889634f, a.weights ? a.weights[t] : 1.f, token, a.lse[t]};
+    else if (a.mode == kBeginForwardFp32) reinterpret_cast<RowState*>(a.rows_c)[pos] = RowState{-INFINITY, 0.f, 0.f};
+  }
+  const T* src = (const T*)a.y + (size_t)t * a.d;
+  T* dst = (T*)a.y_c + (size_t)pos * a.d;
+  if (a.d % 8 == 0) {
+#pragma unroll 8
+    for (int c = lane * 8; c < a.d; c += 64 * 8) {
+      float v[8];
+      ld8(src, c, v);
+      st8(dst, c, v);
     }
+  } else {
+    for (int c = lane; c < a.d; c += 64) dst[c] = src[c];
   }
 }
 
@@ -338,7 +336,7 @@ struct LmCe {
     const LmBegin b{a.y, a.tokens, a.mask, a.row_weights, a.lse, a.loss_rows, ws + p.y_c, at<int32_t>(p.tokens_c), at<int32_t>(p.kept_idx),
                     at<int32_t>(p.row_pos), at<int>(p.cnt), ws + p.rows_c, direct ? nullptr : at<int>(p.counts), a.rows, (int)a.V, (int)a.d,
                     backward ? kBeginBackward : a.dtype == kF32 ? kBeginForwardFp32 : kBeginForward};
-    const dim3 grid((unsigned)((a.rows + 7) / 8)), blk(256);
+    const dim3 grid((unsigned)((a.rows + 3) / 4)), blk(256);
     if (a.dtype == kBF16) hipLaunchKernelGGL(lm_begin_kernel<bf16_t>, grid, blk, 0, s, b);
     else hipLaunchKernelGGL(lm_begin_kernel<float>, grid, blk, 0, s, b);
     return hipGetLastError();
