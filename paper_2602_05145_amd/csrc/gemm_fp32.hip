@@ -469,6 +469,26 @@ hipError_t launch_gemm_fp32(const GemmArgs& a, hipStream_t s) {
   }
 }
 
+// Few rows against a weight that is read from memory: up to 32 rows on tiles no larger than they need be, however many there are, us, small tiles / these:
+// 1 x 128256 x 4008 629 / 414, 14 x 98922 x 2800 421 / 302, 32 x 32000 x 2048 97 / 83.  (The order of the sums is another, so callers ask for it.)
+hipError_t launch_gemm_fp32_few(const GemmArgs& a, hipStream_t s) {
+  Fp32GemmParams p;
+  bool vec;
+  if (a.M > 32 || a.layout != kNT || a.in_dtype != kF32 || a.out_dtype != kF32 || a.M <= 0 || a.N <= 0 || !fp32_params(a, p, vec)) return launch_gemm(a, s);
+  ProfScope ps("gemm_fp32_few", 2.0 * a.M * a.N * (double)a.K, 4.0 * (a.K * (a.M + (double)a.N) + a.M * (double)a.N), s);
+  if (a.m_dev) prof_dynamic(a.m_dev, a.m_off, a.M);
+  const int edge = a.M <= 16 ? 16 : 32;
+  const dim3 grid((unsigned)((a.N + edge - 1) / edge), 1);
+  if (edge == 16) {
+    if (vec) launch_wavek<16, true, true, true, false>(p, grid, s);
+    else launch_wavek<16, true, true, false, false>(p, grid, s);
+  } else {
+    if (vec) launch_wavek<32, true, true, true, false>(p, grid, s);
+    else launch_wavek<32, true, true, false, false>(p, grid, s);
+  }
+  return hipGetLastError();
+}
+
 // A product with a long contraction and few tiles (dy of a loss over a vocabulary): tiles of 64 x 64, the contraction in as many parts as make
 // kFp32PartsTiles of them, each of 128 or more.  Product, its consumer and what else a head's backward pass launches for dy, us, one launch / 8 / 16 /
 // 32 parts: 128 x 256 x 4096 34.7 / 37.9 / 31.5 / 29.9, 32 x 2048 x 32000 234 / 269 / 221 / 203, 100 x 2048 x 32000 481 / 392 / 352 / 357; 1 / 4 /

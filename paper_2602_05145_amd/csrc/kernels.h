@@ -74,6 +74,7 @@ hipError_t launch_gemm_group(const GemmArgs* a, int n, hipStream_t s);  // indep
 constexpr int kMaxFp32Parts = 32, kFp32PartsTiles = 1536;
 int gemm_fp32_parts(int64_t M, int64_t N, int64_t K);
 hipError_t launch_gemm_fp32_parts(const GemmArgs& a, int parts, int64_t stride, hipStream_t s);
+hipError_t launch_gemm_fp32_few(const GemmArgs& a, hipStream_t s);   // fp32, NT, where the rows may be few
 // The LM head's logits z = y W^T (NT, bf16) that are not kept.  Forward: part[t * part_ld + row] = the maximum of z and the sum of
 // exp(z - that) over the t-th kLmColumns columns, label[row] = z[row, tokens[row]] where the launch's columns hold it.
 // Backward: C = weight (exp(z - lse) - [column == token]) in bf16, for columns n0 + c of the vocabulary; the first `zero` columns get 0.

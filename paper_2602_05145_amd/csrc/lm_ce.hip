@@ -279,6 +279,76 @@ __global__ __launch_bounds__(256) void lm_grad_kernel(float* z, int64_t ldz, int
   }
 }
 
+// fp32, up to kFewRows rows: dy and dW in one pass over W.  A wave takes 256 columns and every so many-th four entries of the vocabulary: it reads
+// their weights, adds them to dy by the rows' dz (scalars), and writes dW = scale dz^T y from the rows of y that it holds.  The waves of a block
+// add their dy in LDS; a block's sum is one of the parts that lm_scatter_kernel joins.  Bound by memory: W read, dW written: us, two products / this,
+// 1 x 128256 x 4008 1358 / 845 (4.9 TB/s), 4 x 98922 x 2800 800 / 448.  (With room for 16 rows 14 x 98922 x 2800 took 896, the products 829.)
+constexpr int kFewRows = 4;
+template <bool DW>
+__global__ __launch_bounds__(256) void lm_few_kernel(const float* __restrict__ z, int64_t ldz, int n, const float* __restrict__ w, const float* __restrict__ y,
+                                                     int d, const int* __restrict__ cnt, float scale, float* __restrict__ dy, int64_t stride,
+                                                     float* __restrict__ dw) {
+  typedef float f32x4_t __attribute__((ext_vector_type(4)));
+  __shared__ f32x4_t sm[3][kFewRows][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = min(__builtin_amdgcn_readfirstlane(*cnt), kFewRows);
+  const int col = ((int)blockIdx.x * 64 + lane) * 4, c = min(col, d - 4);   // (d is a multiple of 4)
+  const bool in = col < d;
+  const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4_t acc[kFewRows], ym[DW ? kFewRows : 1];
+#pragma unroll
+  for (int m = 0; m < kFewRows; ++m) {
+    acc[m] = zero;
+    if constexpr (DW) ym[m] = m < rows ? *reinterpret_cast<const f32x4_t*>(y + (size_t)m * d + c) : zero;
+  }
+  const int fours = (n + 3) / 4, step = (int)gridDim.y * 4;
+  auto fetch = [&](f32x4_t (&x)[4], int v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t*>(w + (size_t)min(v + i, n - 1) * d + c));
+  };
+  f32x4_t next[4] = {zero, zero, zero, zero};
+  int q = (int)blockIdx.y * 4 + wave;
+  if (q < fours) fetch(next, q * 4);
+  for (; q < fours; q += step) {
+    const int v = q * 4;
+    f32x4_t k[kFewRows], x[4], g[4] = {zero, zero, zero, zero};
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m) k[m] = *reinterpret_cast<const f32x4_t*>(z + (size_t)max(min(m, rows - 1), 0) * ldz + v);   // (a row is padded to whole 16 bytes)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = next[i];
+    if (q + step < fours) fetch(next, (q + step) * 4);
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m) {
+      if (m < rows) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ki = v + i < n ? k[m][i] : 0.f;
+          acc[m] += ki * x[i];
+          if constexpr (DW) g[i] += ki * ym[m];
+        }
+      }
+    }
+    if constexpr (DW) {
+      if (in) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (v + i < n) __builtin_nontemporal_store(scale * g[i], reinterpret_cast<f32x4_t*>(dw + (size_t)(v + i) * d + c));
+      }
+    }
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m) sm[wave - 1][m][lane] = acc[m];
+  }
+  __syncthreads();
+  if (wave == 0 && in) {
+    float* out = dy + (size_t)blockIdx.y * stride;
+#pragma unroll
+    for (int m = 0; m < kFewRows; ++m)
+      if (m < rows) *reinterpret_cast<f32x4_t*>(out + (size_t)m * d + c) = scale * (((acc[m] + sm[0][m][lane]) + sm[1][m][lane]) + sm[2][m][lane]);
+  }
+}
+
 // compact rows back to their places, zeros elsewhere.  A row is the sum of `parts`, `stride` elements apart.
 template <typename TI, typename TO>
 __global__ __launch_bounds__(256) void lm_scatter_kernel(const TI* __restrict__ src, TO* __restrict__ dst, int d, const int32_t* __restrict__ row_pos, int parts, int64_t stride) {
@@ -373,7 +443,7 @@ hipError_t launch_lm_ce_fwd(const LmCeArgs& a, hipStream_t s) {
   }
   for (int i = 0; i < c.pc.count; ++i) {
     const Piece q = piece_at(c.pc, i);
-    LM_TRY(launch_gemm(c.logits(q), s));
+    LM_TRY(launch_gemm_fp32_few(c.logits(q), s));
     ProfScope ps("lm_ce_stats_fp32", 0, 8.0 * (double)a.rows * q.n, s);
     prof_dynamic(c.cnt(), 0, a.rows);
     hipLaunchKernelGGL(lm_stats_kernel, dim3((unsigned)a.rows), dim3(256), 0, s, c.at<float>(c.p.z), piece_ld(c.pc), (int)q.n0, (int)q.n,
@@ -390,18 +460,29 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
   const int64_t ld = piece_ld(c.pc);
   const bool bf16 = a.dtype == kBF16, to_acc = bf16 && c.pc.count > 1;
   const LmRow* rows = c.at<LmRow>(c.p.rows_c);
-  const int parts = bf16 ? 1 : gemm_fp32_parts(a.rows, a.d, c.pc.width);
+  // very few rows (a single piece then): one pass over W; else each gradient as a product
+  const bool few = !bf16 && a.rows <= kFewRows && a.d % 4 == 0 && a.d <= 16384;
+  const int parts = bf16 ? 1 : few ? (int)std::min<int64_t>(kMaxFp32Parts, (a.V + 63) / 64) : gemm_fp32_parts(a.rows, a.d, c.pc.width);
   const int64_t part_stride = a.rows * a.d;
   for (int i = 0; i < c.pc.count; ++i) {
     const Piece q = piece_at(c.pc, i);
     if (bf16) {
       LM_TRY(launch_gemm_lm_grad(c.logits(q), LmTarget{nullptr, nullptr, 0, nullptr, rows, (int)q.n0, q.zero}, s));
     } else {
-      LM_TRY(launch_gemm(c.logits(q), s));
+      LM_TRY(launch_gemm_fp32_few(c.logits(q), s));
       ProfScope ps("lm_ce_grad_fp32", 0, 8.0 * (double)a.rows * q.n, s);
       prof_dynamic(c.cnt(), 0, a.rows);
       hipLaunchKernelGGL(lm_grad_kernel, dim3((unsigned)a.rows, (unsigned)std::min<int64_t>((q.n + 2047) / 2048, 64)), dim3(256), 0, s, c.at<float>(c.p.z), ld, (int)q.n0, (int)q.n, c.cnt(), rows);
       LM_TRY(hipGetLastError());
+    }
+    if (few) {
+      ProfScope ps("lm_ce_few_fp32", 2.0 * (a.dw ? 2 : 1) * a.rows * q.n * a.d, 4.0 * (a.dw ? 2 : 1) * q.n * a.d, s);
+      const dim3 grid((unsigned)((a.d + 255) / 256), (unsigned)parts);
+      const float *z = c.at<float>(c.p.z), *y = c.at<float>(c.p.y_c);
+      if (a.dw) hipLaunchKernelGGL(lm_few_kernel<true>, grid, dim3(256), 0, s, z, ld, (int)q.n, (const float*)a.w, y, (int)a.d, c.cnt(), a.scale, c.at<float>(c.p.acc), part_stride, (float*)a.dw);
+      else hipLaunchKernelGGL(lm_few_kernel<false>, grid, dim3(256), 0, s, z, ld, (int)q.n, (const float*)a.w, y, (int)a.d, c.cnt(), a.scale, c.at<float>(c.p.acc), part_stride, nullptr);
+      LM_TRY(hipGetLastError());
+      break;
     }
     GemmArgs g = product(kNN, a.rows, a.d, q.n, c.ws + c.p.z, ld, c.piece_w(q), a.d, c.ws + c.p.acc, a.d, a.dtype, to_acc ? kF32 : a.dtype);
     g.m_dev = c.cnt();

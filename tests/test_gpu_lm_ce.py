@@ -143,6 +143,12 @@ def test_every_height_of_tiles(rows, vocab, d, height):
     check(y, w, tokens, mask)
 
 
+# both gradients in one pass up to four rows; not with five, a width that is no multiple of four, or a very wide head
+@pytest.mark.parametrize("rows,vocab,d", [(1, 1, 4), (1, 1001, 256), (2, 63, 260), (3, 4099, 1028), (4, 257, 12), (4, 9001, 2052), (5, 1001, 256), (3, 300, 258), (2, 300, 16388), (17, 13001, 64), (32, 13001, 66)])
+def test_fp32_few_rows(rows, vocab, d):
+    check(*head(rows, vocab, d, "fp32", seed=rows + d), scale=0.5)
+
+
 # the gradient of the hidden states as 32 sums over the vocabulary, of which the last are empty; 5; 2; and one of 4100 rows
 @pytest.mark.parametrize("rows,vocab,d", [(1, 4097, 264), (115, 4096, 256), (70, 16389, 33), (65, 4099, 2056), (333, 700, 64), (130, 300, 72), (4100, 300, 1536)])
 def test_fp32_sums_over_parts_of_the_vocabulary(rows, vocab, d):
