@@ -461,22 +461,25 @@ __device__ __forceinline__ void teacher_logits(TeacherRegs& r, const T* zr, int 
   }
 }
 __device__ __forceinline__ void teacher_load(Teacher& te, const TeacherRegs& r, const DistillArgs& args, int lane) {
+  // a = t / tau less what a row's entries share: their largest one (the difference comes first: it is exact where it is small, whatever the
+  // quotients would be rounded to), or the given log-sum-exp
   float a[kTeacherPer], m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kTeacherPer; ++i) m = fmaxf(m, r.id[i] >= 0 ? r.t[i] : -INFINITY);
+  m = fast_max(m);
   bool says = false;
 #pragma unroll
   for (int i = 0; i < kTeacherPer; ++i) {
-    a[i] = r.id[i] >= 0 ? r.t[i] / args.tau : -INFINITY;
-    says |= !(a[i] == -INFINITY);
-    m = fmaxf(m, a[i]);
+    says |= r.id[i] >= 0 && !(r.t[i] == -INFINITY);
+    a[i] = r.id[i] < 0 ? -INFINITY : args.tlse ? r.t[i] / args.tau - r.lse : (r.t[i] - m) / args.tau;
   }
   const bool any = __any(says);
-  // p = exp(a - L), as exp(a - from) over `sum`: L itself would be rounded to a step of its size
-  float from = r.lse, sum = 1.f;
+  // p = exp(a) over `sum`: its logarithm taken off a would be rounded to a step of a's size
+  float sum = 1.f;
   if (!args.tlse) {
-    from = fast_max(m);
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < kTeacherPer; ++i) s += r.id[i] >= 0 && any ? expf(a[i] - from) : 0.f;
+    for (int i = 0; i < kTeacherPer; ++i) s += r.id[i] >= 0 && any ? expf(a[i]) : 0.f;
     sum = fast_sum(s);
   }
   const float log_sum = logf(sum);
@@ -484,9 +487,9 @@ __device__ __forceinline__ void teacher_load(Teacher& te, const TeacherRegs& r, 
 #pragma unroll
   for (int i = 0; i < kTeacherPer; ++i) {
     const int j = lane + 64 * i;
-    const float p = r.id[i] >= 0 && any ? expf(a[i] - from) / sum : 0.f;
+    const float p = r.id[i] >= 0 && any ? expf(a[i]) / sum : 0.f;
     mass += p;
-    ent += p != 0.f ? p * (a[i] - from - log_sum) : 0.f;
+    ent += p != 0.f ? p * (a[i] - log_sum) : 0.f;
     te.id[j] = r.id[i];
     te.p[j] = p;
     te.z[j] = r.z[i];
