@@ -26,18 +26,6 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t order_pair(float v, int idx) { return ((uint64_t)order_key(v) << 32) | (uint32_t)~idx; }
 
-// 2^(c (z - m)) of values z <= m as 2^(slope z + shift), in one fused step.  Where c m is so large that 1 beside it is nothing (or it has
-// no number: columns masked with the type's lowest value), a power of two takes the place of c, so that slope m is exact, the
-// largest value still gives 1, and the next smaller one 0.  A row of -inf gives 0, +inf and NaN give NaN.
-struct Power { float slope, shift; };
-__device__ __forceinline__ Power power_of(float m, float c) {
-  const float shift = -m * c;
-  if (fabsf(shift) < 1e30f) return Power{c, shift};
-  const uint32_t e = (__float_as_uint(m) >> 23) & 255;   // m is normal, infinite or NaN
-  if (e == 255) return Power{1.f, m == -INFINITY ? 0.f : -m};
-  const float slope = __uint_as_float((127 + 40 + 127 - e) << 23);   // slope m in 2^40 .. 2^41
-  return Power{slope, -m * slope};
-}
 // log-sum-exp of a row's values over the temperature, from their largest one and the sum beside it
 __device__ __forceinline__ float row_lse(const Online& o, float tau) {
   if (o.m == -INFINITY || o.m == INFINITY) return o.s != o.s && o.m == -INFINITY ? o.s : o.m;
@@ -725,7 +713,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
   s = fast_sum(s);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
   __syncthreads();
-  const Online o{m, fast_sum((threadIdx.x & 63) < NT / 64 ? sums[threadIdx.x & 63] : 0.f)};
+  const Online o{m, pw.fix * fast_sum((threadIdx.x & 63) < NT / 64 ? sums[threadIdx.x & 63] : 0.f)};
   const RowGrad g = teacher_finish(te, a, row, masked, o, c, true);
   if (!g.keep) {
     const u32x4_t zero = {0u, 0u, 0u, 0u};
@@ -735,15 +723,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4, 4))) voi
     return;
   }
   float sh = pw.shift;
+  const float f = g.scale * pw.fix;
 #pragma unroll
   for (int i = 0; i < NREG; ++i) {
     turn(i, sh);
-    buf[i] = chunk_grad(buf[i], pw.slope, sh, g.scale);
+    buf[i] = chunk_grad(buf[i], pw.slope, sh, f);
     store(buf[i], c0, i * STEP * (int)sizeof(T));
   }
   for (int i = 0; i < n_lds; ++i) {
     const int col = c0 + (NREG + i) * STEP, nv = V - col;
-    u32x4_t v = chunk_grad(mine[i * NT], pw.slope, sh, g.scale);
+    u32x4_t v = chunk_grad(mine[i * NT], pw.slope, sh, f);
     if (nv < E) {   // padded columns are 0 also where the row's sums are not numbers
 #pragma unroll
       for (int k = 0; k < 4; ++k) {

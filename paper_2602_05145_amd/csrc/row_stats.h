@@ -34,6 +34,20 @@ __device__ __forceinline__ float fast_sum(float v) {
   return last_lane(v);
 }
 
+// 2^(c (z - m)) of values z <= m as fix 2^(slope z + shift), one fused step and the power per value.  shift is -c m rounded, and what that
+// rounding leaves of the exponent of the largest value, the same for all, goes into `fix`.  From |c m| = 2^30 on it would be 32 and more: there a power of
+// two takes the place of c, so that slope m is exact; the largest value gives 1 and the next smaller fp32 number 0, which is less than 2^-64
+// beside it.  (Difference first, (z - m) c, is one step more per value.)  A row of -inf gives 0, +inf and NaN give NaN.
+struct Power { float slope, shift, fix; };
+__device__ __forceinline__ Power power_of(float m, float c) {
+  const float shift = -m * c;
+  if (fabsf(shift) < 0x1p30f) return Power{c, shift, __builtin_amdgcn_exp2f(-fmaf(m, c, shift))};
+  const uint32_t e = (__float_as_uint(m) >> 23) & 255;   // m is normal, infinite or NaN
+  if (e == 255) return Power{1.f, m == -INFINITY ? 0.f : -m, 1.f};
+  const float slope = __uint_as_float((127 + 40 + 127 - e) << 23);   // slope m in 2^40 .. 2^41
+  return Power{slope, -m * slope, 1.f};
+}
+
 // Running (max, sum of 2^(c (z - max))) over eight more values.  The difference comes first: it is 0 for the largest value whatever
 // that is, also where c times it has no number (columns masked with the type's lowest value).
 struct Online { float m, s; };
