@@ -192,14 +192,14 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
   float T_v = __uint_as_float(0x7FC00000u);         // chunks pass unless their maximum is at most this: all, so far
   float m = -INFINITY, s = 0.f;                     // the wave's shift, the lane's sum
   float shift = 0.f;                                // -c m, 0 before any number
-  bool wide = false;                                // whether that is too large to be added to
+  bool wide = false;                                // whether its rounding is too large to stand in the sum: more than 2^-2 of an exponent
   auto raise = [&](float to) {                      // the same in the whole wave
     to = scalar(to);
     if (to > m) {
       s *= m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);   // (before any number the sum is 0, or NaN)
       m = to;
       shift = -m * c;
-      wide = !(fabsf(shift) < 1e30f);
+      wide = !(fabsf(shift) < 0x1p22f);
     }
   };
   auto columns = [&](const Raw8Once<T>& raw, int col, bool tail, float (&v)[8]) {
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(NT, NT == 256 ? (D == 1 ? 8 : 7) : 4) void topk_log
       top[u] = cm;
       if (who[u] && __any(cm > m)) raise(fast_max(cm));
       float part = 0.f;
-      if (wide) {   // (as power_of, which takes registers that are not there)
+      if (wide) {   // (no factor as power_of's: every later raise would meet another rounding)
 #pragma unroll
         for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f((v[j] - m) * c);
       } else {

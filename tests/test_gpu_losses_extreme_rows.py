@@ -59,6 +59,24 @@ TAUS = [1.0, 0.3, 1e-3, 1e-6, 50.0, 1e6]
 SIZES = [300, 4096, 33001, 128256, 200001]
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tau", TAUS)
+@pytest.mark.parametrize("rows", [10, 200, 600])        # each number of threads that a row may have
+@pytest.mark.parametrize("vocab", [300, 33001])
+def test_top_logits(dtype, tau, rows, vocab):
+    z = large_rows(vocab, dtype).repeat(rows // 10, 1)
+    k, tau = 20, as_float(tau)
+    ids, values, lse = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV), torch.empty(rows, device=DEV)
+    B.tide_topk_logits(rows, vocab, z, z.shape[1], k, tau, ids, values, lse, CODE[dtype], stream())
+    sync()
+    want_v, want_i = torch.sort(z[:, :vocab].float(), dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), want_i[:, :k]) and torch.equal(values, want_v[:, :k])
+    _, _, _, _, _, want, tol = statistics(z[:, :vocab], tau)
+    finite = want.abs() < FLOAT_MAX                                       # (the type's lowest value over a small temperature has no fp32 number)
+    assert_within(lse[finite], want[finite], tol[finite], "lse")
+    assert bool((lse[~finite] == -math.inf).all())
+
+
 def distill(z, vocab, ids, t, tlse, tau, train):
     rows, ldz = z.shape
     dtype = "bf16" if z.dtype == torch.bfloat16 else "fp32"
@@ -164,3 +182,23 @@ def test_masked_columns_and_confident_rows(dtype, vocab):
     ids, t = entries(z, vocab, 5, 6)
     ids[2] = torch.arange(5, device=DEV)                # (what -inf masks would cost +inf)
     check_distill(z, vocab, ids, t, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [2, 150, 600])
+@pytest.mark.parametrize("mask", ["low", -1e9, -math.inf])
+def test_log_sum_exp_beside_the_top_logits_of_masked_rows(dtype, rows, mask):
+    """Most columns masked, the others anywhere in the row: the log-sum-exp is that of the others, to their bounds."""
+    vocab, k = 40003, 6
+    mask = torch.finfo(TDT[dtype]).min if mask == "low" else mask
+    z = torch.full((rows, padded(vocab)), mask, device=DEV, dtype=TDT[dtype])
+    left = torch.rand((rows, vocab), device=DEV, generator=gen(7)) < 0.01
+    left[0], left[1] = False, False
+    left[0, vocab - 9:], left[1, :9] = True, True
+    z[:, :vocab] = torch.where(left, 3.0 * torch.randn((rows, vocab), device=DEV, generator=gen(8)), mask).to(TDT[dtype])
+    ids, values, lse = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV), torch.empty(rows, device=DEV)
+    B.tide_topk_logits(rows, vocab, z, z.shape[1], k, 1.0, ids, values, lse, CODE[dtype], stream())
+    sync()
+    _, _, _, _, _, want, tol = statistics(z[:, :vocab], 1.0)
+    assert float(want.abs().max()) < 60
+    assert_within(lse, want, tol, "lse")
