@@ -456,7 +456,8 @@ int tide_distill_train(int64_t rows, int32_t vocab, const void *z, void *dz, int
  *     lse[r] = log-sum-exp of z[r, :],  loss_rows[r] = lse[r] - z[r, tokens[r]]       (both 0 where keep_r is 0)
  * and the backward call, from the same y, w, tokens, mask and that lse,
  *     dy = scale * dz w,  dw = scale * dz^T y,   dz[r, c] = keep_r row_weights[r] (exp(z[r, c] - lse[r]) - [c == tokens[r]])
- * with keep_r = mask[r] != 0 and 0 <= tokens[r] < vocab.  Logits exist only for a piece of the vocabulary at a time (tide_ce_train's
+ * with keep_r = mask[r] != 0 and 0 <= tokens[r] < vocab (lse is one fp32 number per row: from |lse| of some thousands on, its last
+ * step shows in dz).  Logits exist only for a piece of the vocabulary at a time (tide_ce_train's
  * way keeps a block of rows over the whole vocabulary).  Rows that are not kept are not computed: their y may hold anything,
  * they add nothing to dw, and their dy is 0.
  *   y            DEVICE [rows, d], w DEVICE [vocab, d], of dtype TIDE_DTYPE_*; tokens DEVICE int32 [rows], mask DEVICE [rows]

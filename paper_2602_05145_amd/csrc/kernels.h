@@ -78,7 +78,7 @@ hipError_t launch_gemm_fp32_few(const GemmArgs& a, hipStream_t s);   // fp32, NT
 // The LM head's logits z = y W^T (NT, bf16) that are not kept.  Forward: part[t * part_ld + row] = the maximum of z and the sum of
 // exp(z - that) over the t-th kLmColumns columns, label[row] = z[row, tokens[row]] where the launch's columns hold it.
 // Backward: C = weight (exp(z - lse) - [column == token]) in bf16, for columns n0 + c of the vocabulary; the first `zero` columns get 0.
-struct LmRow { float shift, weight; int token; float lse; };   // shift = -lse / ln 2
+struct LmRow { float lse, weight; int token; };
 constexpr int kLmColumns = 256;
 struct LmTarget {
   const int32_t* tokens; float2* part; int64_t part_ld; float* label;

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256) void lm_begin_kernel(LmBegin a) {
     a.row_pos[t] = pos;
     a.kept_idx[pos] = (int32_t)t;
     a.tokens_c[pos] = token;
-    if (a.mode == kBeginBackward) reinterpret_cast<LmRow*>(a.rows_c)[pos] = LmRow{-a.lse[t] * 1.4426950408889634f, a.weights ? a.weights[t] : 1.f, token, a.lse[t]};
+    if (a.mode == kBeginBackward) reinterpret_cast<LmRow*>(a.rows_c)[pos] = LmRow{a.lse[t], a.weights ? a.weights[t] : 1.f, token};
     else if (a.mode == kBeginForwardFp32) reinterpret_cast<RowState*>(a.rows_c)[pos] = RowState{-INFINITY, 0.f, 0.f};
   }
   const T* src = (const T*)a.y + (size_t)t * a.d;

@@ -1,0 +1,66 @@
+"""tide_lm_ce_fwd / tide_lm_ce_bwd on logits that are large, infinite or not numbers, and on vocabularies at the limit."""
+import math
+
+import pytest
+import torch
+
+from paper_2602_05145_amd import binding as B
+from tests.gpu_util import stream, sync
+from tests.loss_util import CODE, DEV, HALF, STEP, TDT, assert_within, gen
+
+pytestmark = pytest.mark.gpu
+
+
+def head(y, w, tokens, want_dw=True):
+    """(lse, loss, dy, dw) of a head whose rows all count."""
+    (rows, d), vocab = y.shape, w.shape[0]
+    code = CODE["bf16" if y.dtype == torch.bfloat16 else "fp32"]
+    ws = torch.empty(B.tide_lm_ce_workspace_bytes(rows, vocab, d, code), dtype=torch.uint8, device=DEV).fill_(0xFF)
+    mask = torch.ones(rows, dtype=torch.uint8, device=DEV)
+    lse, loss = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    dy, dw = torch.empty_like(y), torch.empty_like(w) if want_dw else None
+    B.tide_lm_ce_fwd(rows, vocab, d, y, w, tokens, mask, lse, loss, code, ws, ws.numel(), stream())
+    B.tide_lm_ce_bwd(rows, vocab, d, y, w, tokens, mask, lse, None, 1.0, dy, dw, code, code, ws, ws.numel(), stream())
+    sync()
+    return lse, loss, dy, dw
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("scale", [2.0 ** 8, 2.0 ** 20, 2.0 ** 30, 2.0 ** 33, 2.0 ** 60, 2.0 ** 110])
+@pytest.mark.parametrize("vocab,rows", [(200, 3), (1000, 40), (5003, 300)])
+def test_large_logits(dtype, scale, vocab, rows):
+    """Logits without a rounding (one term each, of few bits), of which every row has one that is the largest by scale / 64 or more: log S is 0 to the last
+    bit of fp32, lse is that logit, the loss its difference to the label's, and dz is 1 there and -1 at the label (0 where they are one)."""
+    d = 8
+    g = gen(vocab)
+    top = torch.randperm(vocab, device=DEV, generator=g)[:d]
+    w = torch.zeros((vocab, d), device=DEV)
+    w[:, 1] = torch.randint(0, 62, (vocab,), device=DEV, generator=g) / 64.0
+    w[top, 1] = 1.0 + torch.arange(d, device=DEV) / 64.0
+    y = torch.zeros((rows, d), device=DEV)
+    y[:, 1] = scale
+    y[1::3, 1] = -scale                                 # the smallest weight is the largest logit then
+    w[:, 1] += 0.5
+    w[top[0], 1] = 0.25
+    z = y.double() @ w.double().T
+    best = z.argmax(1)
+    tokens = torch.randint(0, vocab, (rows,), device=DEV, generator=g)
+    tokens[::2] = best[::2]
+    lse, loss, dy, dw = head(y.to(TDT[dtype]), w.to(TDT[dtype]), tokens.to(torch.int32))
+    at = torch.arange(rows, device=DEV)
+    gap = z[at, best] - z.scatter(1, best[:, None], -math.inf).amax(1)
+    assert float(gap.min()) >= scale / 64
+    # what the other logits leave of a probability: vocab exp(-gap); the lse that the backward call gets is rounded
+    rest = vocab * torch.exp(-gap)
+    assert_within(lse, z[at, best], HALF * z[at, best].abs() + rest + 1e-6, "lse")
+    diff = z[at, best] - z[at, tokens]
+    assert_within(loss, diff, HALF * diff + rest + 1e-6, "loss")
+    dz = torch.zeros_like(z)
+    dz[at, best] += 1.0
+    dz[at, tokens] -= 1.0
+    off = torch.where(tokens == best, 4 * HALF + rest, 4 * HALF + rest + STEP[dtype])    # of each of the one or two that are not nothing
+    want = dz @ w.double()
+    assert_within(dy, want, 1.01 * (2 * off + rest)[:, None] * w.double().abs().max() + STEP[dtype] * want.abs(), "dy")
+    want = dz.T @ y.double()
+    off_sum = (off + rest).max() * rows * scale
+    assert_within(dw, want, 1.01 * off_sum + (rows + 8) * HALF * (dz.abs().T @ y.double().abs()) + STEP[dtype] * (want.abs() + off_sum), "dw")
