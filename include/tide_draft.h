@@ -421,8 +421,8 @@ int tide_ce_train(int64_t rows, int32_t vocab, void *z, int64_t ldz, const int32
  *   ids    DEVICE int32 [rows, k], values DEVICE float [rows, k]: the k largest of columns [0, vocab), the largest first, equal
  *          values (the two zeros too) by ascending column; a NaN counts as larger than every number.  Columns [vocab, ldz) may
  *          hold anything.
- *   lse    DEVICE float [rows] or NULL: the log-sum-exp of z / temperature (-inf for a row of -inf, +inf for one that holds +inf,
- *          NaN for one that holds NaN and no +inf)
+ *   lse    DEVICE float [rows] or NULL: the log-sum-exp of z / temperature (NaN for a row that holds a NaN, else +inf for one that holds
+ *          +inf, else -inf for a row of -inf)
  * 1 <= k <= min(vocab, 128), temperature in [1e-6, 1e6], rows < 2^22; rows may be 0 (the arrays may be NULL then).  Enqueues one kernel
  * and nothing else. */
 int tide_topk_logits(int64_t rows, int32_t vocab, const void *z, int64_t ldz, int32_t k, float temperature,
@@ -434,7 +434,7 @@ int tide_topk_logits(int64_t rows, int32_t vocab, const void *z, int64_t ldz, in
  *     p_j  = exp(a_j - L),  L = log-sum-exp of these a_j, or teacher_lse[r] if teacher_lse is given (the log-sum-exp of the
  *            teacher's WHOLE row over the temperature, as tide_topk_logits gives it: p_j are then the teacher's probabilities,
  *            and what it has outside of its k entries is left out);  P = sum_j p_j
- *     q    = softmax(z[r, 0..vocab) / temperature),  lse[r] = the log-sum-exp of z / temperature
+ *     q    = softmax(z[r, 0..vocab) / temperature),  lse[r] = the log-sum-exp of z / temperature (NaN and infinities: as there)
  *     loss_rows[r] = keep_r temperature^2 sum_j p_j (log p_j - log q[ids_j])
  *     dz[r, c]     = keep_r temperature (P q[c] - sum of p_j with ids_j == c)   for c < vocab, 0 for c in [vocab, ldz)
  * (the gradient of loss_rows[r]; not divided by the number of rows), keep_r = mask[r] != 0 and some entry is above -inf.  A column

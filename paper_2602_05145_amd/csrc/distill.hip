@@ -26,10 +26,10 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 __device__ __forceinline__ uint64_t order_pair(float v, int idx) { return ((uint64_t)order_key(v) << 32) | (uint32_t)~idx; }
 
-// log-sum-exp of a row's values over the temperature, from their largest one and the sum beside it
+// log-sum-exp of a row's values over the temperature, from their largest one and the sum beside it: NaN before +inf before all others
 __device__ __forceinline__ float row_lse(const Online& o, float tau) {
-  if (o.m == -INFINITY || o.m == INFINITY) return o.s != o.s && o.m == -INFINITY ? o.s : o.m;
-  return o.m / tau + logf(o.s);
+  if (o.s != o.s || o.m == INFINITY) return o.s;
+  return o.m == -INFINITY ? o.m : o.m / tau + logf(o.s);
 }
 
 }  // namespace
@@ -512,12 +512,14 @@ __device__ __forceinline__ float teacher_loss(const Teacher& te, int k, const On
 // What a block knows of its row after the statistics, and what remains but for the dense part of the gradient: the loss, and the
 // gradient at the teacher's columns, all of the row's probability on a column in each of its entries.  One barrier.
 struct RowGrad { bool keep; float scale; };   // dz = scale 2^(c (z - max)) off the teacher's columns
-__device__ __forceinline__ RowGrad teacher_finish(Teacher& te, const DistillArgs& a, size_t row, bool masked, const Online& o, float c, bool grad) {
+__device__ __forceinline__ RowGrad teacher_finish(Teacher& te, const DistillArgs& a, size_t row, bool masked, Online o, float c, bool grad) {
   const bool keep = !masked && te.any;
+  const float lse = row_lse(o, a.tau);
+  if (o.m == INFINITY) o.s = NAN;   // no softmax
   const float f = te.mass / o.s;
   if (threadIdx.x < 64) {
     const float loss = keep ? a.tau * a.tau * teacher_loss(te, a.k, o, a.tau, threadIdx.x) : 0.f;
-    if (threadIdx.x == 0) { a.lse[row] = row_lse(o, a.tau); a.loss_rows[row] = loss; }
+    if (threadIdx.x == 0) { a.lse[row] = lse; a.loss_rows[row] = loss; }
   }
   if (grad) {
     const int j = (int)threadIdx.x - 64;   // (the second wave on)

@@ -37,13 +37,13 @@ __device__ __forceinline__ float fast_sum(float v) {
 // 2^(c (z - m)) of values z <= m as fix 2^(slope z + shift), one fused step and the power per value.  shift is -c m rounded, and what that
 // rounding leaves of the exponent of the largest value, the same for all, goes into `fix`.  From |c m| = 2^30 on it would be 32 and more: there a power of
 // two takes the place of c, so that slope m is exact; the largest value gives 1 and the next smaller fp32 number 0, which is less than 2^-64
-// beside it.  (Difference first, (z - m) c, is one step more per value.)  A row of -inf gives 0, +inf and NaN give NaN.
+// beside it.  (Difference first, (z - m) c, is one step more per value.)  A row of -inf gives 0, one with +inf +inf, one with NaN NaN.
 struct Power { float slope, shift, fix; };
 __device__ __forceinline__ Power power_of(float m, float c) {
   const float shift = -m * c;
   if (fabsf(shift) < 0x1p30f) return Power{c, shift, __builtin_amdgcn_exp2f(-fmaf(m, c, shift))};
   const uint32_t e = (__float_as_uint(m) >> 23) & 255;   // m is normal, infinite or NaN
-  if (e == 255) return Power{1.f, m == -INFINITY ? 0.f : -m, 1.f};
+  if (e == 255) return Power{1.f, 0.f, 1.f};
   const float slope = __uint_as_float((127 + 40 + 127 - e) << 23);   // slope m in 2^40 .. 2^41
   return Power{slope, -m * slope, 1.f};
 }
@@ -56,17 +56,17 @@ __device__ __forceinline__ void online_add8(Online& o, const float (&v)[8], floa
 #pragma unroll
   for (int j = 1; j < 8; ++j) cm = fmaxf(cm, v[j]);
   const float nm = fmaxf(o.m, cm);
-  const float sh = nm == -INFINITY ? 0.f : nm;      // nothing but -inf so far: every term is 0
+  const float sh = fabsf(nm) == INFINITY ? 0.f : nm;
   float part = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) part += __builtin_amdgcn_exp2f((v[j] - sh) * c);
-  o.s = (o.m == -INFINITY ? o.s : o.s * __builtin_amdgcn_exp2f((o.m - nm) * c)) + part;   // (before any number: 0, or NaN)
+  o.s = (o.m == nm ? o.s : o.s * __builtin_amdgcn_exp2f((o.m - nm) * c)) + part;
   o.m = nm;
 }
 // of a block of NT threads; every thread gets the result.  sm: NT / 64 pairs.  Two barriers.
 template <int NT>
 __device__ __forceinline__ Online online_block(const Online& o, float c, Online* sm) {
-  auto scaled = [&](const Online& x, float m) { return x.m == -INFINITY ? x.s : x.s * __builtin_amdgcn_exp2f((x.m - m) * c); };   // (a NaN in the sum stays)
+  auto scaled = [&](const Online& x, float m) { return x.m == m ? x.s : x.s * __builtin_amdgcn_exp2f((x.m - m) * c); };   // (a NaN in the sum stays)
   const float wm = fast_max(o.m);
   const float ws = fast_sum(scaled(o, wm));
   __syncthreads();

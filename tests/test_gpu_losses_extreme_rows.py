@@ -202,3 +202,41 @@ def test_log_sum_exp_beside_the_top_logits_of_masked_rows(dtype, rows, mask):
     _, _, _, _, _, want, tol = statistics(z[:, :vocab], 1.0)
     assert float(want.abs().max()) < 60
     assert_within(lse, want, tol, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 5000, 33001, 128256, 200001])
+def test_one_rule_for_infinities_and_nan(dtype, vocab):
+    """The log-sum-exp of a row is NaN if the row holds a NaN, else +inf if it holds +inf, else -inf if it holds nothing else: in every operator, wherever
+    in the row they stand."""
+    inf, nan, at = math.inf, math.nan, [0, 9, vocab // 2, vocab - 1]
+    z = torch.full((24, padded(vocab, 8)), nan, device=DEV, dtype=TDT[dtype])
+    z[:, :vocab] = torch.randn((24, vocab), device=DEV, generator=gen(9)).to(TDT[dtype])
+    row = 0
+    for i in at:
+        for j in at:
+            if i != j:
+                z[row, i], z[row, j] = nan, inf
+                row += 1
+    for i in at:
+        z[row, i], z[row + 1, i] = nan, inf
+        row += 2
+    z[20, :vocab] = -inf
+    z[21, :vocab] = -inf
+    z[21, vocab - 1] = nan
+    z[22, : vocab - 1], z[22, vocab - 1] = -inf, inf
+    z[23, :vocab] = inf
+    z[23, vocab // 3] = nan
+    want = torch.logsumexp(z[:, :vocab].double(), 1)
+    assert torch.equal(want.isnan(), z[:, :vocab].isnan().any(1)) and int((want == inf).sum()) == 5 and int((want == -inf).sum()) == 1
+    k = 5
+    ids, values, lse = torch.empty((24, k), dtype=torch.int32, device=DEV), torch.empty((24, k), device=DEV), torch.empty(24, device=DEV)
+    B.tide_topk_logits(24, vocab, z, z.shape[1], k, 1.0, ids, values, lse, CODE[dtype], stream())
+    t = torch.zeros((24, k), device=DEV)
+    others = torch.arange(k, device=DEV, dtype=torch.int32).repeat(24, 1)
+    for got in (lse, distill(z, vocab, others, t, None, 1.0, False)[0], distill(z, vocab, others, t, None, 1.0, True)[0]):
+        assert_within(got, want.float(), 0.0, "lse")
+    for train in (False, True):                          # (none of these rows has a softmax)
+        _, loss, dz = distill(z, vocab, others, t, None, 1.0, train)
+        assert bool(loss.isnan().all())
+        assert dz is None or bool(dz[:, :vocab].isnan().all()) and bool((dz[:, vocab:] == 0).all())
