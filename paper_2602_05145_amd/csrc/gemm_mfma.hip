@@ -682,7 +682,7 @@ __device__ __forceinline__ void gemm_block(std::conditional_t<ADAM, MfmaAdamPara
         for (int w = 1; w < WAVES_N; ++w) {
           const float2 x = st[w * BM + r];
           const float m = fmaxf(o.x, x.x);
-          if (m > -INFINITY) o.y = o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E) + x.y * __builtin_amdgcn_exp2f((x.x - m) * LOG2E);
+          o.y = m > -INFINITY ? o.y * __builtin_amdgcn_exp2f((o.x - m) * LOG2E) + x.y * __builtin_amdgcn_exp2f((x.x - m) * LOG2E) : o.y + x.y;   // (0, or NaN)
           o.x = m;
         }
         if (m0 + r < p.M) p.lm.part[(size_t)tile_n * p.lm.part_ld + m0 + r] = o;

@@ -64,3 +64,35 @@ def test_large_logits(dtype, scale, vocab, rows):
     want = dz.T @ y.double()
     off_sum = (off + rest).max() * rows * scale
     assert_within(dw, want, 1.01 * off_sum + (rows + 8) * HALF * (dz.abs().T @ y.double().abs()) + STEP[dtype] * (want.abs() + off_sum), "dw")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [5, 300, 2100])      # tiles of 128, and taller ones
+def test_a_logit_that_is_no_number_among_infinite_ones(dtype, rows):
+    """256 columns whose logits are -inf but for one NaN, in any of their quarters: the row's log-sum-exp and loss are NaN, whatever the other columns hold;
+    without the NaN they are those of the other columns."""
+    vocab, d, inf = 1200, 64, math.inf
+    for bad in (None, 256, 300, 350, 400, 511):
+        g = gen(rows)
+        y, w = torch.zeros((rows, d), device=DEV), torch.zeros((vocab, d), device=DEV)
+        y[:, 0], y[:, 1], y[:, 2:] = 1.0, 0.5, torch.randn((rows, d - 2), device=DEV, generator=g)
+        w[:, 2:] = 0.1 * torch.randn((vocab, d - 2), device=DEV, generator=g)
+        w[256:512, 0] = -inf
+        if bad is not None:
+            w[bad, 1] = inf
+        y, w = y.to(TDT[dtype]), w.to(TDT[dtype])
+        tokens = torch.randint(0, 256, (rows,), device=DEV, generator=g).to(torch.int32)
+        code, mask = CODE[dtype], torch.ones(rows, dtype=torch.uint8, device=DEV)
+        ws = torch.empty(B.tide_lm_ce_workspace_bytes(rows, vocab, d, code), dtype=torch.uint8, device=DEV).fill_(0xFF)
+        lse, loss = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        B.tide_lm_ce_fwd(rows, vocab, d, y, w, tokens, mask, lse, loss, code, ws, ws.numel(), stream())
+        sync()
+        if bad is not None:
+            assert bool(lse.isnan().all()) and bool(loss.isnan().all()), bad
+            continue
+        left = torch.cat([w[:256], w[512:]]).double()
+        z = y.double() @ left.T
+        want = torch.logsumexp(z, 1)
+        tol = (d + 2) * HALF * float((y.double().abs() @ left.abs().T).max()) + (vocab / 256 + 64 + 3 * math.log(vocab) + 4) * HALF + 8 * HALF * (math.log(vocab) + 16)
+        assert_within(lse, want, tol, "lse")
+        assert_within(loss, want - z.gather(1, tokens.long()[:, None])[:, 0], 2 * tol, "loss")
