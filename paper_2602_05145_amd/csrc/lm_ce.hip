@@ -33,9 +33,10 @@ int64_t piece_elems(int64_t rows, int64_t V, int dtype) {
   const int64_t budget = ((int64_t)1 << 30) / (int64_t)dtype_size(dtype);
   return std::max(rows * 256, std::min(rows * (int64_t)align_up((size_t)V, 256), budget));
 }
+constexpr int64_t kMostColumns = ((int64_t)1 << 21) - 256;   // bf16 products take rows of fewer than 2^21 elements
 Pieces plan_pieces(int64_t rows, int64_t V, int dtype) {
   const bool by8 = dtype == kBF16;
-  const int64_t most = piece_elems(rows, V, dtype) / rows / 256 * 256, count = (V + most - 1) / most;
+  const int64_t room = piece_elems(rows, V, dtype) / rows / 256 * 256, most = by8 ? std::min(room, kMostColumns) : room, count = (V + most - 1) / most;
   if (count == 1 && by8 && V % 8) return Pieces{V, V / 8 * 8, 2, by8};        // and the rest, at most 7 columns, as a piece of 8
   const int64_t width = (int64_t)align_up((size_t)((V + count - 1) / count), 256);   // (at most `most`)
   return Pieces{V, width, (int)((V + width - 1) / width), by8};

@@ -96,3 +96,62 @@ def test_a_logit_that_is_no_number_among_infinite_ones(dtype, rows):
         tol = (d + 2) * HALF * float((y.double().abs() @ left.abs().T).max()) + (vocab / 256 + 64 + 3 * math.log(vocab) + 4) * HALF + 8 * HALF * (math.log(vocab) + 16)
         assert_within(lse, want, tol, "lse")
         assert_within(loss, want - z.gather(1, tokens.long()[:, None])[:, 0], 2 * tol, "loss")
+
+
+def dz_off(dz, step, lse_tol, ez):
+    """An entry of dz is off by its own rounding and, the probability, by what lse and the logits are off; beside 1 by two half steps more."""
+    return (step + 2 * lse_tol + 2 * ez + 16 * HALF) * dz.abs() + 2 * HALF * (dz.abs() > 0.5)
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 1), ("bf16", 5), ("fp32", 4), ("fp32", 6)])
+@pytest.mark.parametrize("vocab", [2 ** 21 - 1, 2 ** 21 - 8, 2 ** 21 - 64, 2 ** 21 - 256])
+def test_vocabularies_at_the_limit(dtype, rows, vocab):
+    """Row lengths of 2^21 are more than the bf16 products take: the pieces stay below.  dz has one large entry per row, at the label, next to probabilities
+    of 1 / vocab: the references in 64 bits."""
+    d = 8
+    g = gen(vocab % 1000 + rows)
+    y = torch.randn((rows, d), device=DEV, generator=g).to(TDT[dtype])
+    w = torch.randn((vocab, d), device=DEV, generator=g).to(TDT[dtype])
+    tokens = torch.randint(0, vocab, (rows,), device=DEV, generator=g)
+    tokens[0] = vocab - 1
+    lse, loss, dy, dw = head(y, w, tokens.to(torch.int32))
+    step, w64 = STEP[dtype], w.double()
+    want_dw, dw_tol, want_dy = *torch.zeros((2, vocab, d), dtype=torch.float64, device=DEV), torch.empty((rows, d), dtype=torch.float64, device=DEV)
+    for r in range(rows):
+        products = w64 * y[r].double()
+        z = products.sum(1)
+        want = torch.logsumexp(z, 0)
+        ez = (d + 2) * HALF * float(products.abs().sum(1).max())
+        tol = ez + (vocab / 256 + 64 + 3 * math.log(vocab) + 4) * HALF + 8 * HALF * (math.log(vocab) + 16)
+        assert abs(float(lse[r]) - float(want)) <= tol and abs(float(loss[r]) - float(want - z[tokens[r]])) <= 2 * tol, r
+        dz = torch.exp(z - want)
+        dz[tokens[r]] -= 1.0
+        want_dy[r] = (dz[:, None] * w64).sum(0)
+        want_dw += dz[:, None] * y[r].double()
+        dw_tol += (dz_off(dz, step, tol, ez) + (rows + 8) * HALF * dz.abs())[:, None] * y[r].double().abs()
+        off = dz_off(dz, step, tol, ez)
+        dy_tol = ((off + (vocab / 32 + 8) * HALF * dz.abs())[:, None] * w64.abs()).sum(0)
+        assert bool(((dy[r].double() - want_dy[r]).abs() <= dy_tol + step * (want_dy[r].abs() + dy_tol)).all()), r
+    assert bool(((dw.double() - want_dw).abs() <= dw_tol + step * (want_dw.abs() + dw_tol)).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 2 ** 21 - 8), ("bf16", 2 ** 21 - 64), ("fp32", 2 ** 21 - 1), ("fp32", 2 ** 21 - 4)])
+def test_widths_at_the_limit(dtype, d):
+    rows, vocab = 3, 16
+    g = gen(d % 1000)
+    y = torch.randn((rows, d), device=DEV, generator=g).to(TDT[dtype])
+    w = (torch.randn((vocab, d), device=DEV, generator=g) / 1024.0).to(TDT[dtype])
+    tokens = torch.tensor([3, 0, 15], device=DEV)
+    lse, loss, dy, dw = head(y, w, tokens.to(torch.int32))
+    y64, w64, step = y.double(), w.double(), STEP[dtype]
+    products = y64[:, None, :] * w64[None]
+    z, ez = products.sum(2), (d + 2) * HALF * products.abs().sum(2).max()
+    want = torch.logsumexp(z, 1)
+    tol = float(ez) + 100 * HALF * 16
+    assert_within(lse, want, tol, "lse")
+    assert_within(loss, want - z.gather(1, tokens[:, None])[:, 0], 2 * tol, "loss")
+    # (all of a logit's roundings at their worst leave its probability open; at random, 2^17 sums in a row of numbers below 8 make 363 x 8 half steps, 1.8e-4)
+    dz = torch.exp(z - want[:, None])
+    dz[torch.arange(rows, device=DEV), tokens] -= 1.0
+    for got, exact in ((dy, (dz[:, :, None] * w64[None]).sum(1)), (dw, (dz[:, :, None] * y64[:, None, :]).sum(0))):
+        assert float((got.double() - exact).norm() / exact.norm()) < step + 2 * 363 * 8 * HALF
