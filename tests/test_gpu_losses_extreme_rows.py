@@ -8,7 +8,8 @@ import torch
 
 from paper_2602_05145_amd import binding as B
 from tests.gpu_util import stream, sync
-from tests.loss_util import CODE, DEV, HALF, STEP, TDT, assert_within, gen, padded
+from tests.loss_util import CODE, DEV, HALF, STEP, TDT, assert_within, gen, logits, padded
+from tests.test_gpu_topk import _orders
 
 pytestmark = pytest.mark.gpu
 FLOAT_MAX = 3.4028235e38
@@ -240,3 +241,32 @@ def test_one_rule_for_infinities_and_nan(dtype, vocab):
         _, loss, dz = distill(z, vocab, others, t, None, 1.0, train)
         assert bool(loss.isnan().all())
         assert dz is None or bool(dz[:, :vocab].isnan().all()) and bool((dz[:, vocab:] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("given", [False, True], ids=["among k", "teacher_lse"])
+@pytest.mark.parametrize("rows,vocab,k,tau", [(1, 8, 1, 1.0), (3, 100, 100, 0.5), (4, 4095, 16, 1.0), (115, 4096, 16, 1.0), (5, 32001, 64, 1.5), (7, 128256, 32, 2.0),
+                                              (2, 152064, 128, 1.0), (3, 175003, 8, 1.0)])
+def test_ordinary_rows_by_bounds_of_their_own(dtype, given, rows, vocab, k, tau):
+    z = logits(rows, vocab, padded(vocab, 8), dtype, seed=vocab + k)
+    g = gen(vocab)
+    ids = torch.stack([torch.randperm(vocab, device=DEV, generator=g)[:k] for _ in range(rows)]).to(torch.int32)
+    t = 3.0 * torch.randn((rows, k), device=DEV, generator=g) + 4.0
+    check_distill(z, vocab, ids, t, tau, (torch.logsumexp(t.double() / as_float(tau), 1) + 0.4).float() if given else None)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("order", sorted(_orders(64).keys() if torch.cuda.is_available() else ["none"]))
+@pytest.mark.parametrize("rows", [2, 200, 600])
+def test_log_sum_exp_of_every_order(dtype, order, rows):
+    """The sum runs against a shift that rises as the row is read: the orders that raise it often, late or never."""
+    vocab, k = 9000, 37
+    row = _orders(vocab)[order]
+    z = torch.full((rows, padded(vocab)), math.nan, device=DEV, dtype=TDT[dtype])
+    z[0::2, :vocab] = row.to(TDT[dtype])
+    z[1::2, :vocab] = row.flip(0).to(TDT[dtype])
+    ids, values, lse = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV), torch.empty(rows, device=DEV)
+    B.tide_topk_logits(rows, vocab, z, z.shape[1], k, 1.0, ids, values, lse, CODE[dtype], stream())
+    sync()
+    _, _, _, _, _, want, tol = statistics(z[:, :vocab], 1.0)
+    assert_within(lse, want, tol, "lse")
