@@ -280,10 +280,14 @@ __global__ __launch_bounds__(256) void lm_grad_kernel(float* z, int64_t ldz, int
   }
 }
 
-// fp32, up to kFewRows rows: dy and dW in one pass over W.  A wave takes 256 columns and every so many-th four entries of the vocabulary: it reads
+// fp32, up to kFewRows rows of a wide head: dy and dW in one pass over W.  A wave takes 256 columns and every so many-th four entries of the vocabulary: it reads
 // their weights, adds them to dy by the rows' dz (scalars), and writes dW = scale dz^T y from the rows of y that it holds.  The waves of a block
-// add their dy in LDS; a block's sum is one of the parts that lm_scatter_kernel joins.  Bound by memory: W read, dW written: us, two products / this,
-// 1 x 128256 x 4008 1358 / 845 (4.9 TB/s), 4 x 98922 x 2800 800 / 448.  (With room for 16 rows 14 x 98922 x 2800 took 896, the products 829.)
+// add their dy in LDS; a block's sum is one of the parts that lm_scatter_kernel joins.  Bound by memory where there are blocks enough (d / 256 x 32): this kernel
+// alone 836 us at 1 x 128256 x 4008 (4.9 TB/s, 512 blocks), 358 at 2048 wide (5.9 TB/s), 236 at 1024 (4.4), 199 at 256 (1.3: 32 blocks).  With more rows on few blocks
+// it is bound by its own arithmetic, and the two products are faster.  Both gradients, whole calls, us, two products / this: 1 x 128256 x 256
+// 245 / 233, x 512 321 / 262, x 2048 926 / 563, x 4096 1781 / 1139; 2 x 128256 x 512 322 / 339, x 1024 536 / 398; 4 x 128256 x 256 250 / 473, x 1024 539 / 557, x 2048 942 / 696,
+// x 4096 1823 / 1107; dy alone 2 x 128256 x 512 221 / 275, x 1024 319 / 328; 4 x 128256 x 1024 327 / 465, x 2048 558 / 568, x 4096 1122 / 827; over 32000 entries in the same
+// places.  Hence from 512 columns a row on.  (With room for 16 rows 14 x 98922 x 2800 took 896, the products 829.)
 constexpr int kFewRows = 4;
 template <bool DW>
 __global__ __launch_bounds__(256) void lm_few_kernel(const float* __restrict__ z, int64_t ldz, int n, const float* __restrict__ w, const float* __restrict__ y,
@@ -461,8 +465,8 @@ hipError_t launch_lm_ce_bwd(const LmCeArgs& a, hipStream_t s) {
   const int64_t ld = piece_ld(c.pc);
   const bool bf16 = a.dtype == kBF16, to_acc = bf16 && c.pc.count > 1;
   const LmRow* rows = c.at<LmRow>(c.p.rows_c);
-  // very few rows (a single piece then): one pass over W; else each gradient as a product
-  const bool few = !bf16 && a.rows <= kFewRows && a.d % 4 == 0 && a.d <= 16384;
+  // very few rows (a single piece then) of a wide head: one pass over W; else each gradient as a product
+  const bool few = !bf16 && a.rows <= kFewRows && a.d % 4 == 0 && a.d >= 512 * a.rows && a.d <= 16384;
   const int parts = bf16 ? 1 : few ? (int)std::min<int64_t>(kMaxFp32Parts, (a.V + 63) / 64) : gemm_fp32_parts(a.rows, a.d, c.pc.width);
   const int64_t part_stride = a.rows * a.d;
   for (int i = 0; i < c.pc.count; ++i) {
