@@ -349,8 +349,9 @@ __global__ __launch_bounds__(256) void gemm_fp32_group_kernel(Fp32Group g) {
 
 namespace {
 
-// Which kernel.  The large tile when it gives every CU one and has more than 64 rows and columns to fill (NT 16 x 128256 x 2048 595 us with it, 325
-// with the small one; 65 rows 602 / 598); the small one, or the 32-row tile of the split over waves,
+// Which kernel.  The large tile when it gives every CU one and has more than 64 rows and columns to fill (large / small, us: NT 16 x 128256 x 2048 595 / 325,
+// 64 x 128256 590 / 341, 128256 x 16 635 / 364, 128256 x 64 629 / 334; NN in the same order 607 / 331, 598 / 353, 740 / 401, 802 / 341; TN 635 / 350, 643 / 357,
+// 752 / 402, 768 / 352; K of 64 to 1000 alike, nowhere slower; 65 rows 602 / 598); the small one, or the 32-row tile of the split over waves,
 // when it gives three CUs in four one (300 x 2048 x 2048: 54 us with 160 tiles of 64 refused, 79 us with them; 512 x 256 x
 // 4096: 30 us with 128 tiles of 32 refused, 40 with them); else tiles of 16.  Sixteen waves from K = 1024 on
 // (TN 688 x 256 x 512: 8 us with four, 55 with sixteen, whose blocks then have two loads each; NN 128 x 256 x 4096 needs
