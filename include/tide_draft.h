@@ -479,6 +479,86 @@ int tide_lm_ce_bwd(int64_t rows, int32_t vocab, int64_t d, const void *y, const 
                    const uint8_t *mask, const float *lse, const float *row_weights, float scale, void *dy, void *dw, int dw_dtype,
                    int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- A draft of the caller's own: its input, its optimiser, and the round it is for ---- */
+
+/* Embedding: out[r, :] = scale * table[ids[r], :], and zeros where ids[r] is outside [0, vocab) (what pads a batch).
+ *   ids DEVICE int32 [rows], table DEVICE [vocab, d], out DEVICE [rows, d], both of dtype TIDE_DTYPE_*; out overlaps neither
+ * Its gradient: dtable[v, :] = scale * (the sum of dy[r, :] over the rows with ids[r] == v), summed in fp32 in the order of the rows within
+ * fixed pieces: the same inputs give the same bits.  Rows whose id is outside add nothing and their dy may hold anything.
+ *   dy          DEVICE [rows, d] of dtype
+ *   dtable      DEVICE [vocab, d] of dtable_dtype: TIDE_DTYPE_FP32, or dtype.  accumulate 0: overwritten, rows without a token with zeros.  Otherwise added
+ *               to (a table that is the head's weight too has a gradient there already), and rows without a token are not touched.
+ *   workspace   DEVICE, 256-byte aligned, of at least tide_embed_bwd_workspace_bytes(rows, vocab, d) bytes (0 = sizes the calls refuse).  It never falls as
+ *               rows grow, nothing in it has to survive between calls, and calls that overlap need one each.
+ * rows in [0, 2^21] (ids, table, out and dy may be NULL for 0), vocab and d in [1, 2^21), rows * d <= 2^34, scale finite.  Arrays are aligned as their elements
+ * are, no more is asked of them.  Enqueues kernels on `stream` and nothing else. */
+int tide_embed_fwd(int64_t rows, int32_t vocab, int64_t d, const int32_t *ids, const void *table, float scale, void *out,
+                   int dtype, void *stream);
+size_t tide_embed_bwd_workspace_bytes(int64_t rows, int32_t vocab, int64_t d);
+int tide_embed_bwd(int64_t rows, int32_t vocab, int64_t d, const int32_t *ids, const void *dy, float scale, void *dtable,
+                   int dtable_dtype, int accumulate, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One tensor of an AdamW step.  All pointers DEVICE, arrays of n elements, aligned as their elements are; arrays of a call do not overlap. */
+typedef struct tide_adamw_tensor {
+  void *param;         /* of param_dtype */
+  float *master;       /* TIDE_DTYPE_BF16: the fp32 weights, from which param is rounded; else ignored */
+  const void *grad;    /* of grad_dtype */
+  void *m, *v;         /* moments: float for state_bits 32; for 8 one byte each, see below */
+  float *m_scale, *v_scale;   /* state_bits 8: ceil(n / 256) scales each; else ignored */
+  int64_t n;           /* 0 ... 2^34; 0: the pointers may be NULL */
+  float weight_decay;  /* decoupled; 0 for tensors that are not decayed */
+  int32_t param_dtype, grad_dtype, state_bits;
+} tide_adamw_tensor;
+
+/* One AdamW step over all tensors of a list (HOST array, read during the call), with t = step + 1 and g = grad * *grad_scale (DEVICE float, such as
+ * the factor that clips a norm; NULL: grad itself):
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     w = w (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32 on w = master, or param where it is fp32: the update of a training step, for a model of the caller's own.  step: updates applied so far.
+ *
+ * state_bits 8: m and the root of v are kept as e4m3 numbers (OCP, one byte, 448 the largest) times an fp32 scale for each 256 consecutive
+ * elements, 2 + 1/32 bytes per element in place of 8; all-zero bytes and scales are the state of a new tensor.  The step uses the new moments in 32 bits and then
+ * rounds them: to one of the two numbers around, up as often as they lie beyond the lower one, so that changes below a step of the type, which a second moment's
+ * are, add up in the mean over steps.  The random bits come from (seed, t, place in the list, element): the same call gives the same bits.  A moment that is not finite
+ * is kept as NaN and leaves its block alone; a block whose largest magnitude is below 2^-100 is kept as zeros.
+ *
+ * tide_adamw_dev takes the schedule from DEVICE memory, can be captured and replayed: it reads *lr_dev, uses and advances *step_dev, and writes `schedule` (DEVICE
+ * scratch of 4 floats, 16-byte aligned; calls that overlap need one each).  Both forms give the same bits.
+ * beta1 and beta2 in [0, 1), eps and weight_decay finite and >= 0, lr finite.  Enqueues kernels on `stream` and nothing else: one for each 44 tensors. */
+int tide_adamw(int32_t n_tensors, const tide_adamw_tensor *tensors, float lr, float beta1, float beta2, float eps,
+               int64_t step, const float *grad_scale, uint32_t seed, void *stream);
+int tide_adamw_dev(int32_t n_tensors, const tide_adamw_tensor *tensors, const float *lr_dev, int64_t *step_dev, float beta1,
+                   float beta2, float eps, const float *grad_scale, uint32_t seed, float *schedule, void *stream);
+
+/* Verification of drafted tokens (Sec. 3.1: the target checks in one pass what the draft proposed), from given random numbers, such that what is emitted is
+ * distributed as the target alone would have it.  Request b owns target rows cu_rows[b] ... cu_rows[b + 1]: n_b drafted positions and one behind them.  With
+ * tau = temperature[b], p_i the softmax of target row cu_rows[b] + i over tau, q_i that of draft row cu_rows[b] - b + i, x_i = draft_tokens[cu_rows[b] - b + i]
+ * and u_i = uniforms[cu_rows[b] + i]:
+ *     x_i is accepted while u_i q_i(x_i) < p_i(x_i);  accepted[b] = j, how many are
+ *     then one token more is emitted: after a refused x_j from max(0, p_j - q_j), normalised; after all n_b from p_{n_b}: the first column at which the cumulated
+ *     weight is above u_{n_b} (the number of the request's last row) times the whole weight
+ *     tokens[cu_rows[b] + i] = x_i for i < j, the emitted token for i = j, -1 behind it
+ * tau = 0: no sampling; x_i is accepted where it is the first column of the largest logit, which is also what is emitted (draft logits and numbers are not looked at).
+ *   cu_rows      DEVICE int32 [n_requests + 1], from 0, every request at least one row, the last at most `rows`: rows behind it are not looked at, and their
+ *                tokens left as they are.  (Offsets out of order give meaningless numbers but no access outside the arrays.)
+ *   target       DEVICE [rows, ldt], draft DEVICE [rows - n_requests, ldd] of dtype TIDE_DTYPE_*, laid out as in tide_topk_logits; draft NULL: x_i was drawn from
+ *                no distribution but named (q_i(x_i) = 1), and after its refusal the token is drawn from p_j without it
+ *   draft_tokens DEVICE int32 [rows - n_requests] (may be NULL if that is 0).  One outside [0, vocab) ends its request's draft there: n_b is smaller
+ *   temperature  DEVICE float [n_requests], or NULL: 1
+ *   uniforms     DEVICE float [rows], in [0, 1)
+ *   accepted     DEVICE int32 [n_requests], tokens DEVICE int32 [rows]
+ *   workspace    DEVICE, 256-byte aligned, of at least tide_verify_workspace_bytes(rows, n_requests, vocab) bytes (0 = sizes the call refuses, or no rows); nothing in it
+ *                has to survive between calls, and calls that overlap need one each
+ * -inf is a column without probability.  A target row that holds NaN or +inf or nothing above -inf has no distribution: a token there is refused and -1 is
+ * emitted (also where temperature[b] is negative, infinite or NaN).  A draft row of that kind: the token is refused and the target's p_j stands alone, as it does where
+ * max(0, p_j - q_j) is 0 everywhere.  Exponentials and sums are in 64 bits.
+ * 0 <= n_requests <= rows <= 2^20, vocab <= 2^28, rows * vocab <= 2^35.  Enqueues two kernels and nothing else. */
+size_t tide_verify_workspace_bytes(int64_t rows, int32_t n_requests, int32_t vocab);
+int tide_verify_drafts(int64_t rows, int32_t n_requests, int32_t vocab, const int32_t *cu_rows, const void *target, int64_t ldt,
+                       const void *draft, int64_t ldd, const int32_t *draft_tokens, const float *temperature,
+                       const float *uniforms, int32_t *accepted, int32_t *tokens, int dtype,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- Measurement support ----
  * Between tide_profile_start and tide_profile_stop every kernel the library
  * enqueues is bracketed by a pair of HIP events recorded on the caller's stream

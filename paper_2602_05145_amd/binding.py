@@ -46,6 +46,12 @@ class TideTokenInput(C.Structure):
                 ("grad_w_in", C.c_void_p), ("m_w_in", C.c_void_p), ("v_w_in", C.c_void_p), ("master_w_in", C.c_void_p)]
 
 
+class TideAdamwTensor(C.Structure):
+    """tide_adamw_tensor: one tensor of an AdamW step (see make_adamw_tensors)."""
+    _fields_ = [(n, C.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_scale", "v_scale")] + \
+               [("n", C.c_int64), ("weight_decay", C.c_float)] + [(n, C.c_int32) for n in ("param_dtype", "grad_dtype", "state_bits")]
+
+
 class TideError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"tide error {code}: {msg}")
@@ -131,6 +137,21 @@ _lib.tide_lm_ce_fwd.restype = _i32
 _lib.tide_lm_ce_fwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]
 _lib.tide_lm_ce_bwd.restype = _i32
 _lib.tide_lm_ce_bwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _i32, _i32, _vp, _sz, _vp]
+_lib.tide_embed_fwd.restype = _i32
+_lib.tide_embed_fwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _f32, _vp, _i32, _vp]
+_lib.tide_embed_bwd_workspace_bytes.restype = _sz
+_lib.tide_embed_bwd_workspace_bytes.argtypes = [_i64, _i32, _i64]
+_lib.tide_embed_bwd.restype = _i32
+_lib.tide_embed_bwd.argtypes = [_i64, _i32, _i64, _vp, _vp, _f32, _vp, _i32, _i32, _i32, _vp, _sz, _vp]
+_adp = C.POINTER(TideAdamwTensor)
+_lib.tide_adamw.restype = _i32
+_lib.tide_adamw.argtypes = [_i32, _adp, _f32, _f32, _f32, _f32, _i64, _vp, C.c_uint32, _vp]
+_lib.tide_adamw_dev.restype = _i32
+_lib.tide_adamw_dev.argtypes = [_i32, _adp, _vp, _vp, _f32, _f32, _f32, _vp, C.c_uint32, _vp, _vp]
+_lib.tide_verify_workspace_bytes.restype = _sz
+_lib.tide_verify_workspace_bytes.argtypes = [_i64, _i32, _i32]
+_lib.tide_verify_drafts.restype = _i32
+_lib.tide_verify_drafts.argtypes = [_i64, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _sz, _vp]
 _lib.tide_rope.restype = _i32
 _lib.tide_rope.argtypes = [_i32] * 5 + [_f32, _vp, _vp, _i32, _i32, _vp]
 
@@ -150,7 +171,8 @@ EXPORTED = ("tide_last_error", "tide_draft_workspace_bytes", "tide_draft_workspa
             "tide_rmsnorm_fwd", "tide_rmsnorm_bwd_scratch_bytes", "tide_rmsnorm_bwd", "tide_rmsnorm_bwd_static",
             "tide_attention_fwd", "tide_attention_bwd", "tide_rope", "tide_ce_train", "tide_profile_start",
             "tide_profile_stop", "tide_topk_logits", "tide_distill_eval", "tide_distill_train", "tide_lm_ce_workspace_bytes",
-            "tide_lm_ce_fwd", "tide_lm_ce_bwd")
+            "tide_lm_ce_fwd", "tide_lm_ce_bwd", "tide_embed_fwd", "tide_embed_bwd_workspace_bytes", "tide_embed_bwd", "tide_adamw",
+            "tide_adamw_dev", "tide_verify_workspace_bytes", "tide_verify_drafts")
 
 
 def lib():
@@ -444,6 +466,76 @@ def tide_lm_ce_bwd(rows, vocab, d, y, w, tokens, mask, lse, row_weights, scale, 
     """row_weights and dw may be None."""
     rc = _lib.tide_lm_ce_bwd(int(rows), int(vocab), int(d), _ptr(y), _ptr(w), _ptr(tokens), _ptr(mask), _ptr(lse), _ptr(row_weights),
                              float(scale), _ptr(dy), _ptr(dw), dw_dtype, dtype, _ptr(workspace), int(workspace_bytes), stream)
+    return _check(rc) if check else rc
+
+
+def tide_embed_fwd(rows, vocab, d, ids, table, scale, out, dtype, stream, check=True):
+    rc = _lib.tide_embed_fwd(int(rows), int(vocab), int(d), _ptr(ids), _ptr(table), float(scale), _ptr(out), dtype, stream)
+    return _check(rc) if check else rc
+
+
+def tide_embed_bwd_workspace_bytes(rows, vocab, d):
+    return int(_lib.tide_embed_bwd_workspace_bytes(int(rows), int(vocab), int(d)))
+
+
+def tide_embed_bwd(rows, vocab, d, ids, dy, scale, dtable, dtable_dtype, accumulate, dtype, workspace, workspace_bytes, stream, check=True):
+    rc = _lib.tide_embed_bwd(int(rows), int(vocab), int(d), _ptr(ids), _ptr(dy), float(scale), _ptr(dtable), dtable_dtype, int(bool(accumulate)),
+                             dtype, _ptr(workspace), int(workspace_bytes), stream)
+    return _check(rc) if check else rc
+
+
+def make_adamw_tensors(rows):
+    """The list of tide_adamw: per tensor a dict of param, grad, m, v (contiguous torch tensors; the moments float32, or one byte an element
+    beside m_scale and v_scale), master (a bfloat16 param's weights in float32) and weight_decay (0 if left out).  The tensors have to outlive it."""
+    name = lambda t: str(t.dtype)   # noqa: E731
+    code = {"torch.float32": TIDE_DTYPE_FP32, "torch.bfloat16": TIDE_DTYPE_BF16}
+    out = (TideAdamwTensor * len(rows))()
+    for c, t in zip(out, rows):
+        n = t["param"].numel()
+        eight = t.get("m_scale") is not None
+        want = {k: ("torch.float32",) for k in ("master", "m", "v", "m_scale", "v_scale")} | {"param": tuple(code), "grad": tuple(code)}
+        if eight:
+            want |= {k: ("torch.float8_e4m3fn", "torch.uint8") for k in ("m", "v")}
+        for k, types in want.items():
+            x = t.get(k)
+            if x is None:
+                if k in ("param", "grad", "m", "v") or (k == "master" and name(t["param"]) == "torch.bfloat16") or (k == "v_scale" and eight):
+                    raise ValueError(f"{k} is missing")
+                continue
+            if not x.is_contiguous() or name(x) not in types:
+                raise ValueError(f"{k} must be contiguous, of {' or '.join(types)}")
+            least = (n + 255) // 256 if k.endswith("scale") else n
+            if x.numel() < least or (x.numel() != n and not k.endswith("scale")):
+                raise ValueError(f"{k} has {x.numel()} elements, {least} needed")
+            setattr(c, k, x.data_ptr())
+        c.n, c.weight_decay, c.state_bits = n, float(t.get("weight_decay", 0.0)), 8 if eight else 32
+        c.param_dtype, c.grad_dtype = code[name(t["param"])], code[name(t["grad"])]
+    return out
+
+
+def tide_adamw(tensors, lr, beta1, beta2, eps, step, grad_scale, seed, stream, check=True):
+    """tensors: of make_adamw_tensors.  grad_scale may be None."""
+    rc = _lib.tide_adamw(len(tensors), tensors, float(lr), float(beta1), float(beta2), float(eps), int(step), _ptr(grad_scale), int(seed) & 0xFFFFFFFF, stream)
+    return _check(rc) if check else rc
+
+
+def tide_adamw_dev(tensors, lr_dev, step_dev, beta1, beta2, eps, grad_scale, seed, schedule, stream, check=True):
+    """tide_adamw with learning rate (float32) and step count (int64, advanced) on the device; schedule: four floats of scratch."""
+    rc = _lib.tide_adamw_dev(len(tensors), tensors, _ptr(lr_dev), _ptr(step_dev), float(beta1), float(beta2), float(eps), _ptr(grad_scale),
+                             int(seed) & 0xFFFFFFFF, _ptr(schedule), stream)
+    return _check(rc) if check else rc
+
+
+def tide_verify_workspace_bytes(rows, n_requests, vocab):
+    return int(_lib.tide_verify_workspace_bytes(int(rows), int(n_requests), int(vocab)))
+
+
+def tide_verify_drafts(rows, n_requests, vocab, cu_rows, target, ldt, draft, ldd, draft_tokens, temperature, uniforms, accepted, tokens, dtype,
+                       workspace, workspace_bytes, stream, check=True):
+    """draft (then ldd is not looked at) and temperature may be None."""
+    rc = _lib.tide_verify_drafts(int(rows), int(n_requests), int(vocab), _ptr(cu_rows), _ptr(target), int(ldt), _ptr(draft), int(ldd or 0),
+                                 _ptr(draft_tokens), _ptr(temperature), _ptr(uniforms), _ptr(accepted), _ptr(tokens), dtype,
+                                 _ptr(workspace), int(workspace_bytes), stream)
     return _check(rc) if check else rc
 
 

@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/tide_draft.h"
+
 namespace tide {
 
 enum : int { kF32 = 0, kBF16 = 1 };
@@ -273,6 +275,40 @@ hipError_t launch_own_kv_merge_bwd(int64_t T, int S, int nh, int nkv, int dh, co
 // mode 1 acc1 += columns (both then put own_grad [T, 2 nk] into the columns), mode 2 columns += acc1
 hipError_t launch_kv_grad_route(int64_t T, int nq, int nk, void* dqkv, void* acc1, const void* own_grad, int mode,
                                 int dtype, hipStream_t s);
+
+// ---- adamw.hip: AdamW over a caller's list of tensors ------------------------------------------------
+struct AdamwSchedule { float lr, inv_bc1, inv_sqrt_bc2; uint32_t key; };   // of one step; key: what its random bits start from
+struct AdamwListArgs {
+  int n_tensors; const tide_adamw_tensor* tensors;   // HOST
+  float beta1, beta2, eps;
+  float lr; int64_t step;                            // the schedule on the host, or, where `schedule` is set, on the device
+  const float* lr_dev; int64_t* step_dev; AdamwSchedule* schedule;
+  const float* grad_scale;
+  uint32_t seed;
+};
+hipError_t launch_adamw_list(const AdamwListArgs& a, hipStream_t s);
+
+// ---- embedding.hip -----------------------------------------------------------------------------------
+hipError_t launch_embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, const void* table, float scale, void* out, int dtype, hipStream_t s);
+struct EmbedBwdArgs {
+  int64_t rows; int vocab; int64_t d;
+  const int32_t* ids; const void* dy; float scale; void* dtable; int table_dtype, accumulate, dtype;
+  void* workspace;
+};
+size_t embed_bwd_workspace_bytes(int64_t rows, int64_t d);
+hipError_t launch_embed_bwd(const EmbedBwdArgs& a, hipStream_t s);
+
+// ---- verify.hip --------------------------------------------------------------------------------------
+struct VerifyArgs {
+  int64_t rows; int requests; int64_t V;
+  const int32_t* cu;
+  const void* target; int64_t ldt; const void* draft; int64_t ldd;
+  const int32_t* tokens; const float* temperature; const float* uniforms;
+  int32_t *accepted, *out;
+  void* workspace;
+};
+size_t verify_workspace_bytes(int64_t rows, int requests, int64_t V);
+hipError_t launch_verify(const VerifyArgs& a, int dtype, hipStream_t s);
 
 // pure-MFMA rate probe: blocks x 8 waves x iters x 8 MFMAs of 2*32*32*16 flop; sink holds blocks*512 floats
 hipError_t launch_mfma_probe(int blocks, int iters, float* sink, hipStream_t s);

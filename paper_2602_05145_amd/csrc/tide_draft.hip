@@ -1287,6 +1287,122 @@ int tide_lm_ce_bwd(int64_t rows, int32_t vocab, int64_t d, const void* y, const 
   return TIDE_OK;
 }
 
+static bool embed_ok(int64_t rows, int32_t vocab, int64_t d, float scale, int dtype) {
+  if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) { fail(TIDE_ERR_CONFIG, "bad dtype"); return false; }
+  // (a wave of a block of four for 512 columns of a row, and a launch holds fewer than 2^32 threads)
+  if (rows < 0 || rows > ((int64_t)1 << 21) || vocab < 1 || vocab >= (1 << 21) || d < 1 || d >= (1 << 21) || rows * d > ((int64_t)1 << 34)) {
+    fail(TIDE_ERR_CONFIG, "rows must be in [0, 2^21], vocab and d in [1, 2^21), rows * d at most 2^34");
+    return false;
+  }
+  if (!std::isfinite(scale)) { fail(TIDE_ERR_CONFIG, "scale must be finite"); return false; }
+  return true;
+}
+
+int tide_embed_fwd(int64_t rows, int32_t vocab, int64_t d, const int32_t* ids, const void* table, float scale, void* out, int dtype, void* stream) {
+  if (rows != 0 && (!ids || !table || !out)) return fail(TIDE_ERR_NULL, "ids, table and out must not be NULL");
+  if (!embed_ok(rows, vocab, d, scale, dtype)) return TIDE_ERR_CONFIG;
+  const uintptr_t size = dtype == TIDE_DTYPE_BF16 ? 2 : 4;
+  if (((uintptr_t)ids & 3) || ((uintptr_t)table | (uintptr_t)out) & (size - 1)) return fail(TIDE_ERR_CONFIG, "ids, table and out must be aligned as their elements");
+  TIDE_HIP(launch_embed_fwd(rows, vocab, (int)d, ids, table, scale, out, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, (hipStream_t)stream), "embed forward");
+  return TIDE_OK;
+}
+
+size_t tide_embed_bwd_workspace_bytes(int64_t rows, int32_t vocab, int64_t d) {
+  return embed_ok(rows, vocab, d, 1.f, TIDE_DTYPE_FP32) ? embed_bwd_workspace_bytes(rows, d) : 0;
+}
+
+int tide_embed_bwd(int64_t rows, int32_t vocab, int64_t d, const int32_t* ids, const void* dy, float scale, void* dtable, int dtable_dtype, int accumulate, int dtype,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  if ((rows != 0 && (!ids || !dy)) || !dtable || !workspace) return fail(TIDE_ERR_NULL, "NULL argument");
+  if (!embed_ok(rows, vocab, d, scale, dtype)) return TIDE_ERR_CONFIG;
+  if (dtable_dtype != TIDE_DTYPE_FP32 && dtable_dtype != dtype) return fail(TIDE_ERR_CONFIG, "dtable_dtype must be TIDE_DTYPE_FP32 or dtype");
+  const uintptr_t size = dtype == TIDE_DTYPE_BF16 ? 2 : 4, size_of_table = dtable_dtype == TIDE_DTYPE_BF16 ? 2 : 4;
+  if (((uintptr_t)ids & 3) || ((uintptr_t)dy & (size - 1)) || ((uintptr_t)dtable & (size_of_table - 1)))
+    return fail(TIDE_ERR_CONFIG, "ids, dy and dtable must be aligned as their elements");
+  if (((uintptr_t)workspace) & 255) return fail(TIDE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const size_t need = embed_bwd_workspace_bytes(rows, d);
+  if (workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  const EmbedBwdArgs a{rows, vocab, d, ids, dy, scale, dtable, dtable_dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, accumulate, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, workspace};
+  TIDE_HIP(launch_embed_bwd(a, (hipStream_t)stream), "embed backward");
+  return TIDE_OK;
+}
+
+static int adamw(int32_t n_tensors, const tide_adamw_tensor* tensors, AdamwListArgs a, void* stream) {
+  if (n_tensors < 0) return fail(TIDE_ERR_CONFIG, "n_tensors must not be negative");
+  if (n_tensors > 0 && !tensors) return fail(TIDE_ERR_NULL, "tensors is NULL");
+  if (!(a.beta1 >= 0.f && a.beta1 < 1.f && a.beta2 >= 0.f && a.beta2 < 1.f) || !(a.eps >= 0.f) || !std::isfinite(a.eps)) return fail(TIDE_ERR_CONFIG, "invalid AdamW constants");
+  if (((uintptr_t)a.grad_scale) & 3) return fail(TIDE_ERR_CONFIG, "grad_scale must be 4-byte aligned");
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    const tide_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n > ((int64_t)1 << 34)) return fail(TIDE_ERR_CONFIG, "tensor %d: n must be in [0, 2^34]", i);
+    if ((t.param_dtype != TIDE_DTYPE_FP32 && t.param_dtype != TIDE_DTYPE_BF16) || (t.grad_dtype != TIDE_DTYPE_FP32 && t.grad_dtype != TIDE_DTYPE_BF16))
+      return fail(TIDE_ERR_CONFIG, "tensor %d: bad dtype", i);
+    if (t.state_bits != 32 && t.state_bits != 8) return fail(TIDE_ERR_CONFIG, "tensor %d: state_bits must be 32 or 8", i);
+    if (!(t.weight_decay >= 0.f) || !std::isfinite(t.weight_decay)) return fail(TIDE_ERR_CONFIG, "tensor %d: weight_decay must be finite and not negative", i);
+    if (t.n == 0) continue;
+    const bool bf16 = t.param_dtype == TIDE_DTYPE_BF16, eight = t.state_bits == 8;
+    if (!t.param || !t.grad || !t.m || !t.v || (bf16 && !t.master) || (eight && (!t.m_scale || !t.v_scale))) return fail(TIDE_ERR_NULL, "tensor %d: NULL pointer", i);
+    uintptr_t words = bf16 ? (uintptr_t)t.master : (uintptr_t)t.param, halves = bf16 ? (uintptr_t)t.param : 0;
+    (t.grad_dtype == TIDE_DTYPE_BF16 ? halves : words) |= (uintptr_t)t.grad;
+    words |= eight ? (uintptr_t)t.m_scale | (uintptr_t)t.v_scale : (uintptr_t)t.m | (uintptr_t)t.v;
+    if ((words & 3) || (halves & 1)) return fail(TIDE_ERR_CONFIG, "tensor %d: every array must be aligned as its elements", i);
+  }
+  a.n_tensors = n_tensors, a.tensors = tensors;
+  TIDE_HIP(launch_adamw_list(a, (hipStream_t)stream), "adamw");
+  return TIDE_OK;
+}
+
+int tide_adamw(int32_t n_tensors, const tide_adamw_tensor* tensors, float lr, float beta1, float beta2, float eps, int64_t step, const float* grad_scale, uint32_t seed,
+               void* stream) {
+  if (step < 0 || !std::isfinite(lr)) return fail(TIDE_ERR_CONFIG, "step must not be negative, and lr must be finite");
+  AdamwListArgs a{};
+  a.beta1 = beta1, a.beta2 = beta2, a.eps = eps, a.lr = lr, a.step = step, a.grad_scale = grad_scale, a.seed = seed;
+  return adamw(n_tensors, tensors, a, stream);
+}
+
+int tide_adamw_dev(int32_t n_tensors, const tide_adamw_tensor* tensors, const float* lr_dev, int64_t* step_dev, float beta1, float beta2, float eps, const float* grad_scale,
+                   uint32_t seed, float* schedule, void* stream) {
+  if (!lr_dev || !step_dev || !schedule) return fail(TIDE_ERR_NULL, "lr_dev, step_dev and schedule must not be NULL");
+  if (((uintptr_t)lr_dev & 3) || ((uintptr_t)step_dev & 7) || ((uintptr_t)schedule & 15)) return fail(TIDE_ERR_CONFIG, "lr_dev, step_dev and schedule must be 4-, 8- and 16-byte aligned");
+  AdamwListArgs a{};
+  a.beta1 = beta1, a.beta2 = beta2, a.eps = eps, a.grad_scale = grad_scale, a.seed = seed;
+  a.lr_dev = lr_dev, a.step_dev = step_dev, a.schedule = (AdamwSchedule*)schedule;
+  return adamw(n_tensors, tensors, a, stream);
+}
+
+static bool verify_sizes_ok(int64_t rows, int32_t n_requests, int32_t vocab) {
+  // (a block for up to 8192 columns of a row of the target or of the draft, and a launch holds fewer than 2^24 blocks)
+  if (n_requests < 0 || rows < n_requests || rows > (1 << 20) || vocab < 1 || vocab > (1 << 28) || rows * vocab > ((int64_t)1 << 35)) {
+    fail(TIDE_ERR_CONFIG, "0 <= n_requests <= rows <= 2^20, 1 <= vocab <= 2^28 and rows * vocab <= 2^35 are needed");
+    return false;
+  }
+  return true;
+}
+
+size_t tide_verify_workspace_bytes(int64_t rows, int32_t n_requests, int32_t vocab) {
+  return verify_sizes_ok(rows, n_requests, vocab) ? verify_workspace_bytes(rows, n_requests, vocab) : 0;
+}
+
+int tide_verify_drafts(int64_t rows, int32_t n_requests, int32_t vocab, const int32_t* cu_rows, const void* target, int64_t ldt, const void* draft, int64_t ldd,
+                       const int32_t* draft_tokens, const float* temperature, const float* uniforms, int32_t* accepted, int32_t* tokens, int dtype,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  if (!verify_sizes_ok(rows, n_requests, vocab)) return TIDE_ERR_CONFIG;
+  if (n_requests > 0 && (!cu_rows || !target || !uniforms || !accepted || !tokens || !workspace)) return fail(TIDE_ERR_NULL, "NULL argument");
+  if (n_requests > 0 && rows > n_requests && !draft_tokens) return fail(TIDE_ERR_NULL, "draft_tokens is NULL");
+  if (dtype != TIDE_DTYPE_FP32 && dtype != TIDE_DTYPE_BF16) return fail(TIDE_ERR_CONFIG, "bad dtype");
+  if (ldt < vocab || ldt % 8 || ldt > (1 << 28) || (draft && (ldd < vocab || ldd % 8 || ldd > (1 << 28)))) return fail(TIDE_ERR_CONFIG, "bad logit block shape");
+  if (((uintptr_t)target | (uintptr_t)draft) & 15) return fail(TIDE_ERR_CONFIG, "target and draft must be 16-byte aligned");
+  if (((uintptr_t)cu_rows | (uintptr_t)draft_tokens | (uintptr_t)temperature | (uintptr_t)uniforms | (uintptr_t)accepted | (uintptr_t)tokens) & 3)
+    return fail(TIDE_ERR_CONFIG, "arrays of 32-bit numbers must be 4-byte aligned");
+  if (((uintptr_t)workspace) & 255) return fail(TIDE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  const size_t need = verify_workspace_bytes(rows, n_requests, vocab);
+  if (n_requests > 0 && workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  if (n_requests == 0) return TIDE_OK;
+  const VerifyArgs a{rows, n_requests, vocab, cu_rows, target, ldt, rows > n_requests ? draft : nullptr, ldd, draft_tokens, temperature, uniforms, accepted, tokens, workspace};
+  TIDE_HIP(launch_verify(a, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, (hipStream_t)stream), "verify drafts");
+  return TIDE_OK;
+}
+
 }  // extern "C"
 
 // ---- optional per-launch profiler (prof.h) --------------------------------------------------------
