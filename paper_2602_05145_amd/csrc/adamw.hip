@@ -44,7 +44,7 @@ __host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, int64_t t) 
 }
 
 __device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int count) {
-  if (count >= 8) return load_loose<1, u32x2>(p);
+  if (count >= 8) return LDX(u32x2_of_bytes, p);
   u32x2 c = {0, 0};
 #pragma unroll
   for (int j = 0; j < 8; ++j)
@@ -52,7 +52,7 @@ __device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int count) {
   return c;
 }
 __device__ __forceinline__ void store_codes(uint8_t* p, int count, const u32x2& c) {
-  if (count >= 8) return store_loose<1>(p, c);
+  if (count >= 8) { STX(u32x2_of_bytes, p, c); return; }
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     if (j < count) p[j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
@@ -79,8 +79,8 @@ __device__ __forceinline__ u32x2 encode(const float (&x)[8], const uint32_t (&co
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]) < INFINITY ? fabsf(x[j]) : 0.f);
   top = max_of_32(top);
-  if (!(top >= 0x1p-100f)) top = 0.f;   // (448 / top has to be a number)
-  const float factor = top > 0.f ? kTop / top : 0.f;
+  if (!(top >= 0x1p-100f)) top = 0.f;   // (1 / top has to be a number)
+  const float factor = top > 0.f ? (1.f / top) * kTop : 0.f;   // (what this rounds moves the largest by a few of the 2^20 that `coin` covers)
   scale = top * (1.f / kTop);
   u32x2 c = {0, 0};
 #pragma unroll

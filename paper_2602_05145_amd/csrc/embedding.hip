@@ -96,7 +96,7 @@ template <typename T> struct Row8;   // eight elements as loaded
 template <> struct Row8<bf16_t> {
   u32x4 a;
   __device__ __forceinline__ void load(const bf16_t* p, int count) {
-    if (count >= 8) { a = load_loose<2, u32x4>(p); return; }
+    if (count >= 8) { a = LDX(u32x4_of_halves, p); return; }
     a = u32x4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -110,7 +110,7 @@ template <> struct Row8<bf16_t> {
 template <> struct Row8<float> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const float* p, int count) {
-    if (count >= 8) { a = load_loose<4, f32x4>(p), b = load_loose<4, f32x4>(p + 4); return; }
+    if (count >= 8) { a = LDX(f32x4_of_floats, p), b = LDX(f32x4_of_floats, p + 4); return; }
     a = b = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -4,29 +4,39 @@
 
 namespace tide {
 
-template <typename V, int A> struct __attribute__((packed, aligned(A))) Loose { V v; };
-template <int A, typename V> __device__ __forceinline__ V load_loose(const void* p) { return reinterpret_cast<const Loose<V, A>*>(p)->v; }
-template <int A, typename V> __device__ __forceinline__ void store_loose(void* p, const V& v) { reinterpret_cast<Loose<V, A>*>(p)->v = v; }
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef f32x4 __attribute__((aligned(4))) f32x4_of_floats;
+typedef u32x4 __attribute__((aligned(2))) u32x4_of_halves;
+typedef u32x2 __attribute__((aligned(1))) u32x2_of_bytes;
+#ifdef TIDE_NTL
+#define LDX(T, p) __builtin_nontemporal_load(reinterpret_cast<const T*>(p))
+#else
+#define LDX(T, p) (*reinterpret_cast<const T*>(p))
+#endif
+#ifdef TIDE_NTS
+#define STX(T, p, v) __builtin_nontemporal_store(v, reinterpret_cast<T*>(p))
+#else
+#define STX(T, p, v) (*reinterpret_cast<T*>(p) = (v))
+#endif
 
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const f32x4 a = load_loose<4, f32x4>(p), b = load_loose<4, f32x4>(p + 4);
+  const f32x4 a = LDX(f32x4_of_floats, p), b = LDX(f32x4_of_floats, p + 4);
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
 }
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  store_loose<4>(p, f32x4{x[0], x[1], x[2], x[3]});
-  store_loose<4>(p + 4, f32x4{x[4], x[5], x[6], x[7]});
+  STX(f32x4_of_floats, p, (f32x4{x[0], x[1], x[2], x[3]}));
+  STX(f32x4_of_floats, p + 4, (f32x4{x[4], x[5], x[6], x[7]}));
 }
 __device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
-  const u32x4 a = load_loose<2, u32x4>(p);
+  const u32x4 a = LDX(u32x4_of_halves, p);
 #pragma unroll
   for (int j = 0; j < 4; ++j) x[2 * j] = __uint_as_float(a[j] << 16), x[2 * j + 1] = __uint_as_float(a[j] & 0xFFFF0000u);
 }
 __device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
-  store_loose<2>(p, u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])});
+  STX(u32x4_of_halves, p, (u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])}));
 }
 template <typename T> __device__ __forceinline__ void load_some(const T* p, int count, float (&x)[8]) {
   if (count >= 8) return load8(p, x);

@@ -1,7 +1,14 @@
 // Drafted tokens verified against the target's logits: include/tide_draft.h has the formulas.
 //
 // Whether a token is accepted, and which one a cumulated distribution gives at a number, is decided at a border: with a vocabulary of 10^5 columns, sums that are
-// off by 1e-7 pick another token for one number in forty.  So exponentials and sums are in 64 bits, off by 1e-12 at most.
+// off by 1e-7 pick another token for one number in forty.  So the exponentials and sums that decide are in 64 bits, off by 1e-12 at most.  They take 17 operations a column, twice what
+// memory leaves time for, and few rows need them: one of a request's is the one behind the accepted tokens, and of the others a sum in 32 bits says which side of the border a number
+// is on unless it is within 3e-5 of it.
+//   1 verify_stats    every row's maximum and sum of exponentials by parts of its columns, in 32 bits; in 64 where all rows are few
+//   2 verify_decide   how many tokens are accepted (a number next to its border: by sums of its rows in 64 bits on the spot), what is written but for the emitted token
+//   3 verify_sums     sums in 64 bits of the rows that token is drawn from, where a draft's is taken off (not where 1 made them)
+//   4 verify_weights  their weights by parts, down to 512 columns
+//   5 verify_pick     the part and in it the column in which the cumulated weight goes over the border
 #include <algorithm>
 
 #include "kernels.h"
@@ -12,15 +19,23 @@ namespace tide {
 namespace {
 
 constexpr int kStep = 2048;       // columns that a block of 256 threads takes at a time, eight a thread
-constexpr int kMaxPicks = 64;     // parts of a row that weights are summed over: one lane each
+constexpr int kMaxPicks = 64;     // parts of a row that a block each sums: one lane each where they are joined
+constexpr int kUnits = 8;         // finer parts that a wave each weighs, for each lane where they are cumulated: 512 columns up to 2^18 of them
+constexpr int kMaxUnits = 64 * kUnits;
 constexpr double kLog2eD = 1.4426950408889634074;
+constexpr double kNear = 0x1p-15;   // what a comparison of sums in 32 bits may be off, see rough_ok
 
 struct Part { double sum; float top; int32_t at; };   // sum of exp((z - top) / tau); the first column that holds the top (without sampling)
+struct Sums { double p, q; };   // of a part of the rows that the emitted token is drawn from
+// where it is drawn from: rows of the target and (or -1) of the draft, their largest values, the column that is taken off (or -1), where it goes; p's sum of exponentials,
+// log2(e) / tau and -1200 over that
+struct Draw { int64_t p, q; float top_p, top_q; int taken, to; double sum, c, least; float number; };
 
-// 2^t for -1200 <= t <= 1: n = round(t), and on the rest f in [-1/2, 1/2] the polynomial 1 + f r(f) of least relative error (8.1e-13) with seven degrees
-// in r, by exchange of its extreme points.  2^0 is 1.
-__device__ __forceinline__ double pow2(double t) {
-  const double n = rint(t), f = t - n;
+// 2^(c d) for -1200 <= c d <= 0.  The product rounded to an integer n is what the first step leaves in the low bits of k; on the rest f in [-1/2, 1/2] stands the polynomial
+// 1 + f r(f) of least relative error (8.1e-13) with seven degrees in r, by exchange of its extreme points.  d = 0 gives 1.
+__device__ __forceinline__ double power(double d, double c) {
+  constexpr double kShift = 0x1.8p52;
+  const double k = fma(d, c, kShift), f = fma(d, c, kShift - k);
   double r = 1.3178933490506645e-06;
   r = fma(r, f, 1.530915617496178e-05);
   r = fma(r, f, 0.00015403825462319016);
@@ -29,33 +44,39 @@ __device__ __forceinline__ double pow2(double t) {
   r = fma(r, f, 0.05550410935266197);
   r = fma(r, f, 0.2402265069811059);
   r = fma(r, f, 0.6931471805482124);
-  return ldexp(fma(r, f, 1.0), (int)n);
+  return ldexp(fma(r, f, 1.0), __double2loint(k));
 }
-// exp((z - top) / tau) of numbers z <= top as 2^(slope z + shift): one fused step, and what its rounded shift leaves, the same for all, in `fix`.  From |c top| = 2^40
-// on, where next to the largest value the next smaller fp32 number lies 2^16 and more below in the exponent, a power of two takes the place of c: its shift is exact, the
-// largest value gives 1 and all others 0, as they should.
+// exp((z - top) / tau), c = log2(e) / tau: the difference comes first, so that the largest value gives 1 whatever it is.
 struct Scale {
-  double slope, shift, fix;
-  __device__ __forceinline__ Scale(double c, double top) : slope(c), shift(-c * top), fix(1.0) {
-    if (fabs(shift) < 0x1p40) {
-      fix = pow2(-fma(c, top, shift));
-    } else {
-      int e;
-      frexp(top, &e);
-      slope = ldexp(1.0, 41 - e);
-      shift = -slope * top;
-    }
-  }
-  __device__ __forceinline__ double of(float z) const { return pow2(fmax(fma((double)z, slope, shift), -1200.0)); }
+  double c, top, least;
+  __device__ __forceinline__ Scale(double c_, float top_) : Scale(c_, top_, -1200.0 / c_) {}
+  __device__ __forceinline__ Scale(double c_, float top_, double least_) : c(c_), top((double)top_), least(least_) {}
+  __device__ __forceinline__ double of(float z) const { return power(fmax((double)z - top, least), c); }     // z <= top, or -inf
+  __device__ __forceinline__ double near(float z) const { return power((double)z - top, c); }                // where -1000 <= c (z - top); a NaN stays
 };
-__device__ __forceinline__ double beside(float z, float top, double c) { return pow2(fmax(((double)z - (double)top) * c, -1200.0)); }   // z <= top, not both infinite
 __device__ __forceinline__ bool usable(float top) { return fabsf(top) < INFINITY; }   // (a NaN is not)
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// The sum over the lanes up to this one and over all of a wave, on the vector unit alone.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)bits, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(bits >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+__device__ __forceinline__ double up_to(double v) {
+  v += dpp<0x111, 0xf>(v);   // from 1, 2, 4 and 8 lanes below in a row of 16
+  v += dpp<0x112, 0xf>(v);
+  v += dpp<0x114, 0xf>(v);
+  v += dpp<0x118, 0xf>(v);
+  v += dpp<0x142, 0xa>(v);   // the row below's last lane, in rows 1 and 3; then the lower half's, in the upper
+  return v + dpp<0x143, 0xc>(v);
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {   // the same lane for the whole wave
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)bits, lane), hi = __builtin_amdgcn_readlane((int)(bits >> 32), lane);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum(double v) { return lane_of(up_to(v), 63); }
 
 // The rows of request b: `rows` of the target, of which the last has no drafted token, and drafts from draft row `first`.  Offsets that are out of order are cut to
 // what is there.
@@ -73,20 +94,63 @@ __device__ __forceinline__ float tau_of(const float* temperature, int b) {
   return t >= 0.f && t < INFINITY ? t : __uint_as_float(0x7FC00000u);
 }
 
-template <typename T>
-__device__ __forceinline__ void load_row8(const T* row, int64_t col, int64_t V, float (&z)[8]) {   // -inf behind the last column
-  if (col < V) ld8(row, (size_t)col, z);
+__device__ __forceinline__ void opaque(Raw8<bf16_t>& r) { asm volatile("" : "+v"(r.a.x), "+v"(r.a.y), "+v"(r.a.z), "+v"(r.a.w)); }
+__device__ __forceinline__ void opaque(Raw8<float>&) {}
+__device__ __forceinline__ void cut(Raw8<bf16_t>& r, int count) {   // -inf from the count-th element on
+  uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) z[j] = col + j < V ? z[j] : -INFINITY;
+  for (int j = 0; j < 4; ++j) w[j] = count > 2 * j + 1 ? w[j] : count > 2 * j ? (w[j] & 0xFFFFu) | 0xFF800000u : 0xFF80FF80u;
+  r.a = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void cut(Raw8<float>& r, int count) {
+  float z[8];
+  r.get(z);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z[j] = j < count ? z[j] : -INFINITY;
+  r.a = make_float4(z[0], z[1], z[2], z[3]), r.b = make_float4(z[4], z[5], z[6], z[7]);
 }
 
-// Of U * 2048 columns of one row: the largest value and the sum of exponentials beside it.
+template <typename T>
+struct Eight {   // columns of a row, -inf behind the last one
+  Raw8<T> raw;
+  __device__ __forceinline__ void load(const T* row, int64_t col, int64_t V) { raw.load(row, (size_t)min(col, (V - 1) / 8 * 8)); }
+  __device__ __forceinline__ void get(int64_t col, int64_t V, float (&z)[8]) {
+    if (__ballot(col + 8 > V)) cut(raw, (int)min(max(V - col, (int64_t)0), (int64_t)8));
+    raw.get(z);
+  }
+};
+// Whether all of a wave's numbers are close enough to the largest that no power of them has to be held back.
+__device__ __forceinline__ bool all_near(const Scale& e, const float (&z)[8]) {
+  const float least = fminf(fminf(fminf(z[0], z[1]), fminf(z[2], z[3])), fminf(fminf(z[4], z[5]), fminf(z[6], z[7])));
+  return !__ballot(((double)least - e.top) * e.c < -1000.0);
+}
+
+// The request that a row belongs to, the first that ends behind it, by a wave; a.requests where there is none.
+__device__ __forceinline__ int owner_of(const VerifyArgs& a, int64_t row, bool of_target, int lane) {
+  for (int b0 = 0; b0 < a.requests; b0 += 256) {
+    int end[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) end[u] = a.cu[min(b0 + 64 * u + lane, a.requests - 1) + 1];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = b0 + 64 * u + lane;
+      const unsigned long long ends = __ballot(k < a.requests && (int64_t)end[u] - (of_target ? 0 : k + 1) > row);
+      if (ends) return b0 + 64 * u + __ffsll(ends) - 1;
+    }
+  }
+  return a.requests;
+}
+
+// Temperatures for which sums in 32 bits are good to kNear / 4.  An exponent c (z - top) takes three roundings, |t| 2^-23.4 of its power; with up to 2^28 columns those that
+// make a difference have |t| <= 28 and so 2^-18.6.  A thread adds 64 of them, 2^-18.  At the ends of fp32 c itself loses bits.
+__device__ __forceinline__ bool rough_ok(float tau) { return tau >= 0x1p-100f && tau <= 0x1p100f; }
+
+// Of U * 2048 columns of one row: the largest value and the sum of exponentials beside it, in 64 bits.
 template <typename T, int U>
-__global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyArgs a, int parts, Part* __restrict__ stats, int* __restrict__ tickets) {
+__global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyArgs a, int parts, Part* __restrict__ stats) {
   __shared__ double sums[4];
   __shared__ float tops[4];
   __shared__ int places[4];
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.requests; i += (int64_t)gridDim.x * 256) tickets[i] = 0;
   const int64_t unit = blockIdx.x / parts;
   const int part = (int)(blockIdx.x % parts);
   const bool of_target = unit < a.rows;
@@ -97,306 +161,557 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyArgs a, i
   Raw8<T> raw[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) raw[u].load(base, (size_t)min(col + u * kStep, (a.V - 1) / 8 * 8));
-  int b = a.requests;   // the first request that ends behind the row
-  for (int b0 = 0; b0 < a.requests; b0 += 64) {
-    const int k = b0 + lane;
-    const unsigned long long ends = __ballot(k < a.requests && (int64_t)a.cu[min(k, a.requests - 1) + 1] - (of_target ? 0 : k + 1) > row);
-    if (ends) {
-      b = b0 + __ffsll(ends) - 1;
-      break;
-    }
-  }
+  const int b = owner_of(a, row, of_target, lane);
   if (b >= a.requests) return;
   const float tau = tau_of(a.temperature, b);
   if (!(tau >= 0.f) || (tau == 0.f && !of_target)) return;
-  float z[U][8], top = -INFINITY;
-  bool odd = false;   // holds a NaN
+  if ((int64_t)(part + 1) * (U * kStep) > a.V) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) cut(raw[u], (int)min(max(a.V - col - u * kStep, (int64_t)0), (int64_t)8));
+  }
+  float top = -INFINITY, least = INFINITY;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    raw[u].get(z[u]);
+    float z[8];
+    raw[u].get(z);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[u][j] = col + u * kStep + j < a.V ? z[u][j] : -INFINITY;
-      odd |= z[u][j] != z[u][j];
-      top = fmaxf(top, z[u][j]);
+    for (int j = 0; j < 8; j += 2) {
+      top = fmaxf(fmaxf(top, z[j]), z[j + 1]);   // (a NaN is passed over)
+      least = fminf(fminf(least, z[j]), z[j + 1]);
     }
+    opaque(raw[u]);   // (taken apart again below: to keep the numbers would take twice the registers)
   }
-  top = __ballot(odd) ? __uint_as_float(0x7FC00000u) : fast_max(top);
+  top = fast_max(top);
+  auto odd = [&] {   // whether the wave holds a NaN
+    bool is = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float z[8];
+      raw[u].get(z);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) is |= z[j] != z[j];
+    }
+    return __ballot(is) != 0;
+  };
   Part* out = stats + unit * parts + part;
   if (tau == 0.f) {
     int at = 0x7FFFFFFF;
 #pragma unroll
-    for (int u = U - 1; u >= 0; --u)
+    for (int u = U - 1; u >= 0; --u) {
+      float z[8];
+      raw[u].get(z);
 #pragma unroll
-      for (int j = 7; j >= 0; --j) at = z[u][j] == top ? (int)(col + u * kStep + j) : at;
+      for (int j = 7; j >= 0; --j) at = z[j] == top ? (int)(col + u * kStep + j) : at;
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
-    if (lane == 0) tops[wave] = top, places[wave] = at;
+    const double nan = odd() ? __builtin_nan("") : 0.0;
+    if (lane == 0) tops[wave] = top, places[wave] = at, sums[wave] = nan;
     __syncthreads();
     if (threadIdx.x == 0) {
-      for (int w = 1; w < 4; ++w) {
-        if (!(top == top)) break;
-        if (!(tops[w] <= top)) top = tops[w], at = places[w];
+      for (int w = 1; w < 4; ++w)
+        if (tops[w] > top) top = tops[w], at = places[w];
         else if (tops[w] == top) at = min(at, places[w]);
-      }
-      *out = Part{0.0, top, at};
+      *out = Part{sums[0] + sums[1] + sums[2] + sums[3], top, at};
     }
     return;
   }
   const double c = kLog2eD / (double)tau;
   double sum = 0.0;
-  if (usable(top)) {
-    const Scale e(c, (double)top);
+  if (!usable(top)) {
+    sum = odd() ? __builtin_nan("") : 0.0;
+  } else {
+    const Scale e(c, top);
+    if (!__ballot(((double)least - e.top) * c < -1000.0)) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        float z[8];
+        raw[u].get(z);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += e.of(z[u][j]);
-    sum = wave_sum(sum) * e.fix;
+        for (int j = 0; j < 8; ++j) sum += e.near(z[j]);
+      }
+      sum = wave_sum(sum);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float z[8];
+        raw[u].get(z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += e.of(z[j]);
+      }
+      sum = odd() ? __builtin_nan("") : wave_sum(sum);
+    }
   }
   if (lane == 0) sums[wave] = sum, tops[wave] = top;
   __syncthreads();
   if (threadIdx.x == 0) {
-    float m = tops[0];
-    for (int w = 1; w < 4; ++w) m = !(tops[w] <= m) ? tops[w] : m;   // (a NaN stays: nothing is at least it)
-    for (int w = 0; w < 4; ++w)
-      if (!(tops[w] == tops[w])) m = tops[w];
+    const float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const Scale all(c, m);
     sum = 0.0;
-    if (usable(m))
-      for (int w = 0; w < 4; ++w) sum += tops[w] == -INFINITY ? 0.0 : sums[w] * beside(tops[w], m, c);
+    for (int w = 0; w < 4; ++w) sum += usable(tops[w]) && usable(m) ? sums[w] * all.of(tops[w]) : sums[w];
     *out = Part{sum, m, 0};
+  }
+}
+
+// The same in 32 bits, of `columns` columns.
+template <typename T>
+__global__ __launch_bounds__(256) void verify_rough_stats_kernel(const VerifyArgs a, int parts, int columns, Part* __restrict__ stats) {
+  __shared__ Online joined[4];
+  __shared__ float tops[4];
+  __shared__ int places[4], odds[4];
+  const int64_t unit = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x % parts);
+  const bool of_target = unit < a.rows;
+  const int64_t row = of_target ? unit : unit - a.rows;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int b = owner_of(a, row, of_target, lane);
+  if (b >= a.requests) return;
+  const float tau = tau_of(a.temperature, b);
+  if (!(tau >= 0.f) || (tau == 0.f && !of_target)) return;
+  const int first = part * columns, n = (int)min((int64_t)columns, a.V - first);
+  const T* z_row = (of_target ? (const T*)a.target + row * a.ldt : (const T*)a.draft + row * a.ldd) + first;
+  Part* out = stats + unit * parts + part;
+  if (tau > 0.f) {
+    const float c = (float)(kLog2eD / (double)tau);
+    const Online o = online_block<256>(row_stats<T, 256, true>(z_row, n, c), c, joined);
+    if (threadIdx.x == 0) *out = Part{(double)o.s, o.m, 0};
+    return;
+  }
+  float top = -INFINITY;
+  int at = 0x7FFFFFFF;
+  bool odd = false;
+  for (int col = threadIdx.x * 8; col < n; col += kStep) {
+    float z[8];
+    ld8(z_row, (size_t)col, z);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (col + j < n) {
+        odd |= z[j] != z[j];
+        if (z[j] > top) top = z[j], at = first + col + j;   // (the first of a thread's, which ascend)
+      }
+  }
+  const float most = fast_max(top);
+  at = top == most ? at : 0x7FFFFFFF;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
+  const bool any_odd = __ballot(odd) != 0;
+  if (lane == 0) tops[wave] = most, places[wave] = at, odds[wave] = any_odd;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    top = tops[0], at = places[0];
+    for (int w = 1; w < 4; ++w)
+      if (tops[w] > top) top = tops[w], at = places[w];
+      else if (tops[w] == top) at = min(at, places[w]);
+    *out = Part{odds[0] | odds[1] | odds[2] | odds[3] ? __builtin_nan("") : 0.0, top, at};
   }
 }
 
 // A whole row from its parts, by one wave: `ok` where it has a distribution
 struct Row { double sum; float top; int at; bool ok; };
 __device__ __forceinline__ Row join_row(const Part* p, int parts, double c, bool sampled, int lane) {
-  float top = -INFINITY;
-  bool odd = false;
-  for (int k = lane; k < parts; k += 64) odd |= p[k].top != p[k].top, top = fmaxf(top, p[k].top);
+  Part mine{0.0, -INFINITY, 0x7FFFFFFF};
+  if (lane < parts) mine = p[lane];
+  float top = mine.top;
+  for (int k = lane + 64; k < parts; k += 64) top = fmaxf(top, p[k].top);
   top = fast_max(top);
-  Row r{0.0, top, 0x7FFFFFFF, !__ballot(odd) && usable(top)};
-  if (!r.ok) return r;
-  for (int k = lane; k < parts; k += 64) {
-    if (p[k].top == -INFINITY) continue;
-    if (sampled) r.sum += p[k].sum * beside(p[k].top, top, c);
-    else if (p[k].top == top) r.at = min(r.at, p[k].at);
-  }
-  if (sampled) r.sum = wave_sum(r.sum);
-  else
+  const Scale e(c, top);
+  Row r{0.0, top, 0x7FFFFFFF, usable(top)};
+  auto add = [&](const Part& x) {
+    r.sum += sampled && usable(x.top) && r.ok ? x.sum * e.of(x.top) : x.sum;
+    if (x.top == top) r.at = min(r.at, x.at);
+  };
+  add(mine);
+  for (int k = lane + 64; k < parts; k += 64) add(p[k]);
+  r.sum = wave_sum(r.sum);
+  r.ok = r.ok && r.sum == r.sum;
+  if (!sampled) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) r.at = min(r.at, __shfl_xor(r.at, o, 64));
+  }
   return r;
 }
 
-// Each of a request's blocks finds out how many drafted tokens are accepted and sums the weights of its columns for the token behind them; the last one to finish
-// picks that token.
+template <int WAVES>
+__device__ __forceinline__ double block_sum(double v, double* red) {   // every thread gets it; two barriers
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double all = 0.0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) all += red[w];
+  return all;
+}
+
+// One block a request.  With rough sums (not `exact`) a comparison next to its border is made again with the sums of its rows in 64 bits.
 template <typename T>
-__global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyArgs a, int parts, int picks, int64_t span, const Part* __restrict__ stats,
-                                                          double* __restrict__ weights, int* __restrict__ tickets) {
-  __shared__ int stop, ended, finishes, last_seen, chosen;
-  __shared__ Row joined[2];
-  __shared__ double partial[4];
-  __shared__ double before_s, border_s;
-  __shared__ int64_t begin_s;
-  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t drafted = a.rows - a.requests, V = a.V;
-  const View v = view_of(a.cu, b, a.rows, drafted);
+__global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, int parts, int picks, bool exact, const Part* __restrict__ stats, Sums* __restrict__ sums,
+                                                            Draw* __restrict__ draws) {
+  constexpr int kAhead = 32;   // drafted positions that are looked at together
+  __shared__ Row of_p[kAhead + 1], of_q[kAhead];
+  __shared__ int stop_s, token_s, unsure_s;
+  __shared__ double red[8];
+  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t V = a.V;
+  const View v = view_of(a.cu, b, a.rows, a.rows - a.requests);
+  if (threadIdx.x == 0) draws[b].p = -1;
   if (!v.any) {
-    if (pick == 0 && threadIdx.x == 0) a.accepted[b] = 0;
+    if (threadIdx.x == 0) a.accepted[b] = 0;
     return;
   }
   const float tau = tau_of(a.temperature, b);
-  const bool sampled = tau > 0.f;
+  const bool sampled = tau > 0.f, drawn = sampled && a.draft;
   const double c = kLog2eD / (double)tau;
   const Part* of_target = stats + v.row0 * parts;
-  const Part* of_draft = a.draft ? stats + (a.rows + v.first) * parts : nullptr;
+  const Part* of_draft = stats + (a.rows + v.first) * parts;
   const T* z_target = (const T*)a.target + v.row0 * a.ldt;
-  const T* z_draft = a.draft ? (const T*)a.draft + v.first * a.ldd : nullptr;
-  if (threadIdx.x == 0) stop = tau == tau ? v.n : 0, ended = 0x7FFFFFFF;
-  __syncthreads();
+  const T* z_draft = (const T*)a.draft + v.first * a.ldd;
+  auto whole = [&](const T* row, float top) {   // the sum of a row in 64 bits, by the block
+    const Scale e(c, top);
+    double sum = 0.0;
+    for (int64_t col = threadIdx.x * 8; col < V; col += 512 * 8) {
+      Eight<T> raw;
+      float z[8];
+      raw.load(row, col, V);
+      raw.get(col, V, z);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += e.of(z[k]);
+    }
+    return block_sum<8>(sum, red);
+  };
   // a token is accepted if u q(x) < p(x); one that is no token ends the draft
+  int j = 0, i0 = 0, taken = -1;
+  bool refused = false;   // a token was: what it was drawn from is taken off
   if (tau == tau)
-    for (int i = wave; i < v.n; i += 4) {
-      const int x = a.tokens[v.first + i];
-      const bool token = x >= 0 && x < V;
-      const Row p = join_row(of_target + (int64_t)i * parts, parts, c, sampled, lane);
-      bool takes = token && p.ok;
-      if (!sampled) takes = takes && x == p.at;
-      else if (takes) {
-        const double px = beside(ldf(z_target, (size_t)(i * a.ldt + x)), p.top, c) / p.sum;
-        double qx = 1.0;
-        if (a.draft) {
-          const Row q = join_row(of_draft + (int64_t)i * parts, parts, c, true, lane);
-          qx = q.ok ? beside(ldf(z_draft, (size_t)(i * a.ldd + x)), q.top, c) / q.sum : __builtin_nan("");
+    for (;; i0 += kAhead) {
+      const int n = min(kAhead, v.n - i0), rows = min(kAhead + 1, v.n + 1 - i0), tasks = rows + (drawn ? n : 0);
+      int x = -1;
+      float zp = 0.f, zq = 0.f, u = 0.f;
+      if (threadIdx.x < n) {
+        const int64_t i = i0 + threadIdx.x;
+        x = a.tokens[v.first + i];
+        u = a.uniforms[v.row0 + i];
+        if (sampled && x >= 0 && x < V) {
+          zp = ldf(z_target, (size_t)(i * a.ldt + x));
+          if (drawn) zq = ldf(z_draft, (size_t)(i * a.ldd + x));
         }
-        takes = (double)a.uniforms[v.row0 + i] * qx < px;
       }
-      if (!takes && lane == 0) {
-        atomicMin(&stop, i);
-        if (!token) atomicMin(&ended, i);
+      for (int t = wave; t < tasks; t += 8) {
+        const bool of_other = t >= rows;
+        const int k = of_other ? t - rows : t;
+        const Row r = join_row((of_other ? of_draft : of_target) + (int64_t)(i0 + k) * parts, parts, c, sampled, lane);
+        if (lane == 0) (of_other ? of_q : of_p)[k] = r;
       }
+      int sure = 0;   // positions in front are decided
+      for (bool again = true; again;) {
+        __syncthreads();
+        if (wave == 0) {
+          const bool token = x >= 0 && x < V;
+          bool takes = token && lane < n, unsure = false;
+          if (takes) {
+            const Row p = of_p[lane];
+            takes = p.ok;
+            if (!sampled) takes = takes && x == p.at;
+            else if (takes) {
+              const double px = Scale(c, p.top).of(zp) / p.sum;
+              double qx = 1.0;
+              if (drawn) qx = of_q[lane].ok ? Scale(c, of_q[lane].top).of(zq) / of_q[lane].sum : __builtin_nan("");
+              const double left = (double)u * qx;
+              takes = left < px;
+              unsure = !exact && lane >= sure && (rough_ok(tau) ? fabs(left - px) <= kNear * px : left == left);
+            }
+          }
+          const unsigned long long not_taken = __ballot(lane < n && (!takes || unsure));
+          const int first = not_taken ? __ffsll(not_taken) - 1 : n;
+          if (lane == first && first < n) token_s = token ? x : -1, unsure_s = unsure;
+          if (lane == 0) {
+            stop_s = first;
+            if (first == n) unsure_s = 0;
+          }
+        }
+        __syncthreads();
+        again = unsure_s;
+        if (again) {
+          const int k = stop_s;
+          const double sp = whole(z_target + (int64_t)(i0 + k) * a.ldt, of_p[k].top);
+          const double sq = drawn ? whole(z_draft + (int64_t)(i0 + k) * a.ldd, of_q[k].top) : 0.0;
+          if (threadIdx.x == 0) {
+            of_p[k].sum = sp;
+            if (drawn) of_q[k].sum = sq;
+          }
+          sure = k + 1;
+        }
+      }
+      j = i0 + stop_s;
+      if (stop_s < n) {
+        taken = token_s;
+        refused = taken >= 0;
+      }
+      if (stop_s < n || i0 + n == v.n) break;
+      __syncthreads();
     }
-  __syncthreads();
-  const int j = stop;
-  const bool refused = j < v.n && ended != j;   // a token was: what it was drawn from is taken off
-  if (wave < 2) {
-    Row r{0.0, 0.f, -1, false};
-    if (tau == tau) {
-      if (wave == 0) r = join_row(of_target + (int64_t)j * parts, parts, c, sampled, lane);
-      else if (refused && sampled && a.draft) r = join_row(of_draft + (int64_t)j * parts, parts, c, true, lane);
-    }
-    if (lane == 0) joined[wave] = r;
+  Row p{0.0, 0.f, -1, false}, q = p;
+  if (tau == tau) p = of_p[j - i0];
+  if (drawn && refused) q = of_q[j - i0];
+  const bool told = !sampled || !p.ok;   // the emitted token is known, or there is none
+  for (int64_t i = threadIdx.x; i <= v.n; i += 512)
+    if (i != j || told) a.out[v.row0 + i] = i < j ? a.tokens[v.first + i] : i == j && p.ok ? p.at : -1;
+  if (threadIdx.x == 0) a.accepted[b] = j;
+  if (told) return;
+  if (threadIdx.x == 0) {
+    // (named and not drawn: the token itself is taken off)
+    draws[b] = Draw{v.row0 + j, q.ok ? v.first + j : -1, p.top, q.top, refused && !a.draft ? taken : -1, (int)(v.row0 + j), p.sum, c, -1200.0 / c, a.uniforms[v.row0 + v.n]};
   }
-  __syncthreads();
-  const Row p = joined[0], q = joined[1];
-  auto tell = [&](int token) {   // by the whole block
-    for (int64_t i = threadIdx.x; i <= v.n; i += 256) a.out[v.row0 + i] = i < j ? a.tokens[v.first + i] : i == j ? token : -1;
-    if (threadIdx.x == 0) a.accepted[b] = j;
-  };
-  if (!sampled || !p.ok) {
-    if (pick == 0) tell(p.ok ? p.at : -1);
-    return;
+  if (exact && threadIdx.x < picks) {
+    Sums* s = sums + (int64_t)b * kMaxPicks + threadIdx.x;
+    s->p = threadIdx.x == 0 ? p.sum : 0.0;
+    s->q = threadIdx.x == 0 && q.ok ? q.sum : 0.0;
   }
-  const Scale ep(c, (double)p.top), eq(c, q.ok ? (double)q.top : 0.0);
-  const double ip = ep.fix / p.sum, iq = q.ok ? eq.fix / q.sum : 0.0;
-  const T* zp = z_target + (int64_t)j * a.ldt;
-  const T* zq = q.ok ? z_draft + (int64_t)j * a.ldd : nullptr;
-  const int64_t taken = refused && !a.draft ? a.tokens[v.first + j] : -1;
-  auto weigh = [&](int64_t col, bool alone, double (&w)[8]) {   // of eight columns; alone: the target's probabilities
+}
+
+// What a request's token is drawn from, as the last three kernels go over it.
+template <typename T>
+struct Source {
+  const T *zp, *zq;   // zq: NULL where nothing is taken off
+  Scale ep, eq;
+  double ip, iq;      // 1 / the whole sums; without a draft's row 1, as weights are on any scale
+  int taken;
+  int64_t V;
+  __device__ __forceinline__ Source(const VerifyArgs& a, const Draw& d)
+      : zp((const T*)a.target + d.p * a.ldt), zq(d.q >= 0 ? (const T*)a.draft + d.q * a.ldd : nullptr), ep(d.c, d.top_p, d.least),
+        eq(d.c, d.top_q, d.least), ip(1.0), iq(0.0), taken(d.taken), V(a.V) {}
+  __device__ __forceinline__ void join(const Sums* s, int picks, int lane) {   // by every wave
+    if (!zq) return;
+    const Sums mine = lane < picks ? s[lane] : Sums{0.0, 0.0};
+    ip = 1.0 / wave_sum(mine.p), iq = 1.0 / wave_sum(mine.q);
+  }
+  struct Columns { Eight<T> p, q; };
+  __device__ __forceinline__ void load(int64_t col, Columns& x) const {
+    x.p.load(zp, col, V);
+    if (zq) x.q.load(zq, col, V);
+  }
+  __device__ __forceinline__ void weigh(int64_t col, Columns& x, double (&w)[8]) const {   // by a whole wave
     float z[8], y[8];
-    load_row8(zp, col, V, z);
-    if (zq && !alone) load_row8(zq, col, V, y);
+    x.p.get(col, V, z);
+    if (all_near(ep, z)) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      w[k] = ep.of(z[k]) * ip;
-      if (zq && !alone) w[k] = fmax(w[k] - eq.of(y[k]) * iq, 0.0);
-      else if (!alone && col + k == taken) w[k] = 0.0;
+      for (int k = 0; k < 8; ++k) w[k] = ep.near(z[k]) * ip;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = ep.of(z[k]) * ip;
+    }
+    if (zq) {
+      x.q.get(col, V, y);
+      if (all_near(eq, y)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.near(y[k]), iq, w[k]), 0.0);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.of(y[k]), iq, w[k]), 0.0);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = col + k == taken ? 0.0 : w[k];
+    }
+  }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a, int picks, int64_t span, const Draw* __restrict__ draws, Sums* __restrict__ sums) {
+  __shared__ double red[8];
+  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
+  const Draw d = draws[b];
+  if (d.p < 0 || d.q < 0) return;
+  const Source<T> s(a, d);
+  double p = 0.0, q = 0.0;
+  const int64_t to = min((pick + 1) * span, a.V);
+  auto add = [](const Scale& e, const float (&z)[8], double& sum) {
+    if (all_near(e, z)) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += e.near(z[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum += e.of(z[k]);
     }
   };
-  double sum = 0.0;
-  const int64_t from = pick * span, to = min(from + span, V);
-  for (int64_t base = from; base < to; base += kStep) {
+  for (int64_t base = pick * span; base < to; base += kStep) {
     const int64_t col = base + threadIdx.x * 8;
-    if (col >= V) continue;
-    double w[8];
-    weigh(col, false, w);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum += w[k];
+    typename Source<T>::Columns x;
+    s.load(col, x);
+    float z[8];
+    x.p.get(col, a.V, z);
+    add(s.ep, z, p);
+    x.q.get(col, a.V, z);
+    add(s.eq, z, q);
   }
-  sum = wave_sum(sum);
-  if (lane == 0) partial[wave] = sum;
+  p = wave_sum(p);
+  q = wave_sum(q);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = p, red[4 + (threadIdx.x >> 6)] = q;
   __syncthreads();
   if (threadIdx.x == 0) {
-    __hip_atomic_store(weights + (int64_t)b * kMaxPicks + pick, partial[0] + partial[1] + partial[2] + partial[3], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // released with the ticket, so that whoever sees it sees the sum
-    finishes = __hip_atomic_fetch_add(tickets + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == picks - 1;
+    Sums* out = sums + (int64_t)b * kMaxPicks + pick;
+    out->p = red[0] + red[1] + red[2] + red[3];
+    out->q = red[4] + red[5] + red[6] + red[7];
   }
-  __syncthreads();
-  if (!finishes) return;
-  // the first part whose cumulated weight goes over the border; none: the last that weighs anything
-  bool alone = false;
-  if (wave == 0) {
-    double mine = lane < picks ? __hip_atomic_load(weights + (int64_t)b * kMaxPicks + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0, upto = mine;
+}
+
+// A wave weighs units: the 512 columns that it takes of each step, or `per` steps of them.
+template <typename T>
+__global__ __launch_bounds__(256) void verify_weights_kernel(const VerifyArgs a, int picks, int64_t span, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
+                                                             double* __restrict__ weights) {
+  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Draw d = draws[b];
+  if (d.p < 0) return;
+  Source<T> s(a, d);
+  const int64_t unit = (int64_t)per * 512, to = min((pick + 1) * span, a.V);
+  typename Source<T>::Columns x;
+  s.load(pick * span + wave * unit + lane * 8, x);   // (under way while the sums are joined)
+  s.join(sums + (int64_t)b * kMaxPicks, picks, lane);
+  for (int64_t first = pick * span + wave * unit; first < to; first += 4 * unit) {
+    double sum = 0.0;
+    const int64_t end = min(first + unit, to);
+    for (int64_t base = first; base < end; base += 512) {
+      if (base > pick * span + wave * unit) s.load(base + lane * 8, x);
+      double w[8];
+      s.weigh(base + lane * 8, x, w);
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double x = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += x;
+      for (int k = 0; k < 8; ++k) sum += w[k];
     }
-    const double all = __shfl(upto, 63, 64);
-    const double border = fmax((double)a.uniforms[v.row0 + v.n] * all, 0.0);
-    const unsigned long long over = __ballot(upto > border), some = __ballot(mine > 0.0);
-    const int at = over ? __ffsll(over) - 1 : some ? 63 - __clzll(some) : -1;
-    const double front = __shfl(upto - mine, max(at, 0), 64);
-    if (lane == 0) {
-      // nothing weighs anything (a number of 1 and more refused what both distributions agree on): from the target's alone
-      begin_s = at < 0 ? -1 : at * span;
-      before_s = at < 0 ? 0.0 : front;
-      border_s = at < 0 ? fmax((double)a.uniforms[v.row0 + v.n], 0.0) : border;
-      chosen = 0x7FFFFFFF, last_seen = -1;
-    }
+    sum = wave_sum(sum);
+    if (lane == 0) weights[(int64_t)b * kMaxUnits + first / unit] = sum;
   }
-  __syncthreads();
-  alone = begin_s < 0;
-  const int64_t begin = alone ? 0 : begin_s, finish = alone ? V : min(begin + span, V);
-  double before = before_s;
-  const double border = border_s;
-  for (int64_t base = begin; base < finish; base += kStep) {
-    const int64_t col = base + threadIdx.x * 8;
-    double w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (col < V) weigh(col, alone, w);
-    double mine = 0.0;
-    int top = -1;
+}
+
+// One wave a request: the first unit whose cumulated weight goes over the border (none: the last that weighs anything), and in it the first column.
+template <typename T>
+__global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a, int picks, int units, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
+                                                         const double* __restrict__ weights) {
+  const int b = blockIdx.x, lane = threadIdx.x;
+  const Draw d = draws[b];
+  if (d.p < 0) return;
+  Source<T> s(a, d);
+  s.join(sums + (int64_t)b * kMaxPicks, picks, lane);
+  const double number = fmax((double)d.number, 0.0);
+  double w[8], own = 0.0;
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) {
+    const int at = lane * kUnits + k;
+    w[k] = at < units ? weights[(int64_t)b * kMaxUnits + at] : 0.0;
+    own += w[k];
+  }
+  double upto = up_to(own), border = number * lane_of(upto, 63), before = 0.0;
+  const int64_t unit = (int64_t)per * 512;
+  int64_t begin = -1, finish = a.V;
+  // where the cumulated weight goes over the border: of eight weights of each lane, the first or, where there is none, the last that is not 0
+  auto crossing = [&](double front, int& at, double& in_front) {
+    double run = front + (upto - own);
+    int found = -1, seen = -1;
+    double found_front = 0.0, seen_front = 0.0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      mine += w[k];
-      top = w[k] > 0.0 ? (int)(col + k) : top;
-    }
-    double upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double x = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += x;
-    }
-    if (lane == 63) partial[wave] = upto;
-    if (top >= 0) atomicMax(&last_seen, top);
-    __syncthreads();
-    double front = before;
-    for (int k = 0; k < wave; ++k) front += partial[k];
-    double run = front + (upto - mine);
-    if (front + upto > border) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        run += w[k];
-        if (run > border && w[k] > 0.0) {
-          atomicMin(&chosen, (int)(col + k));
-          break;
-        }
+      if (w[k] > 0.0) {
+        if (found < 0 && run + w[k] > border) found = k, found_front = run;
+        seen = k, seen_front = run;
       }
+      run += w[k];
     }
-    before += partial[0] + partial[1] + partial[2] + partial[3];
-    __syncthreads();
-    if (chosen != 0x7FFFFFFF) break;
+    const unsigned long long over = __ballot(found >= 0), some = __ballot(seen >= 0);
+    const int who = over ? __ffsll(over) - 1 : some ? 63 - __clzll(some) : 0;
+    at = some ? who * 8 + __builtin_amdgcn_readlane(over ? found : seen, who) : -1;
+    in_front = lane_of(over ? found_front : seen_front, who);
+    return over != 0;
+  };
+  int at;
+  crossing(0.0, at, before);
+  if (at >= 0) {
+    begin = at * unit, finish = min(begin + unit, a.V);
+  } else {   // nothing weighs anything (a number of 1 and more refused what both distributions agree on): from the target's alone
+    border = number * d.sum * s.ip, before = 0.0, begin = 0;
+    s.zq = nullptr, s.taken = -1;
   }
-  tell(chosen != 0x7FFFFFFF ? chosen : last_seen);
+  int64_t token = -1;
+  for (int64_t base = begin; base < finish; base += 512) {
+    const int64_t col = base + lane * 8;
+    typename Source<T>::Columns x;
+    s.load(col, x);
+    s.weigh(col, x, w);
+    own = 0.0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) own += w[k];
+    upto = up_to(own);
+    double front;
+    const bool over = crossing(before, at, front);
+    if (at >= 0) token = base + at;
+    if (over) break;
+    before += lane_of(upto, 63);
+  }
+  if (lane == 0) a.out[d.to] = (int)token;
 }
 
 int64_t parts_of(int64_t V, int u) { return (V + (int64_t)u * kStep - 1) / ((int64_t)u * kStep); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// Up to so many columns in all rows the exact sums are made at once, which saves a launch: 5M 20.7 us beside 23.8 with sums in 32 bits first, 10M 25.1 / 24.9, 18M 34.8 / 30.4,
+// 295M 304 / 178 (bf16).
+constexpr int64_t kFewColumns = 10 << 20;
 
 }  // namespace
 
 size_t verify_workspace_bytes(int64_t rows, int requests, int64_t V) {
-  return up256((size_t)(2 * rows - requests) * (size_t)parts_of(V, 1) * sizeof(Part)) + up256((size_t)requests * kMaxPicks * sizeof(double)) +
-         up256((size_t)requests * sizeof(int));
+  return up256((size_t)requests * kMaxPicks * sizeof(Sums)) + up256((size_t)requests * kMaxUnits * sizeof(double)) + up256((size_t)requests * sizeof(Draw)) +
+         up256((size_t)(2 * rows - requests) * (size_t)parts_of(V, 1) * sizeof(Part));
 }
 
-hipError_t launch_verify(const VerifyArgs& a, int dtype, hipStream_t s) {
+template <typename T>
+static hipError_t verify(const VerifyArgs& a, hipStream_t s) {
   char* ws = (char*)a.workspace;
-  double* weights = (double*)ws;
-  int* tickets = (int*)(ws + up256((size_t)a.requests * kMaxPicks * sizeof(double)));
-  Part* stats = (Part*)((char*)tickets + up256((size_t)a.requests * sizeof(int)));
+  Sums* sums = (Sums*)ws;
+  double* weights = (double*)(ws + up256((size_t)a.requests * kMaxPicks * sizeof(Sums)));
+  Draw* draws = (Draw*)((char*)weights + up256((size_t)a.requests * kMaxUnits * sizeof(double)));
+  Part* stats = (Part*)((char*)draws + up256((size_t)a.requests * sizeof(Draw)));
   const int64_t units = a.rows + (a.draft ? a.rows - a.requests : 0);
-  const int u = units * parts_of(a.V, 4) >= 2048 ? 4 : units * parts_of(a.V, 2) >= 2048 ? 2 : 1;
+  const bool exact = units * a.V <= kFewColumns;
+  // exact: registers hold up to 8192 columns of a block; else a block goes over up to 32768 (16384 and 65536: 1 % slower), less where that leaves CUs idle
+  int u = exact ? 4 : 16;
+  while (u > 1 && units * parts_of(a.V, u) < 2048) u /= 2;
   const int64_t parts = parts_of(a.V, u);
   {
-    ProfScope ps("verify_stats", 4.0 * (double)units * a.V, (double)units * a.V * dtype_size(dtype), s);
+    ProfScope ps("verify_stats", 4.0 * (double)units * a.V, (double)units * a.V * sizeof(T), s);
     const dim3 grid((unsigned)(units * parts)), block(256);
-#define TIDE_VERIFY(T, U) hipLaunchKernelGGL((verify_stats_kernel<T, U>), grid, block, 0, s, a, (int)parts, stats, tickets)
-    if (dtype == kBF16) { if (u == 4) TIDE_VERIFY(bf16_t, 4); else if (u == 2) TIDE_VERIFY(bf16_t, 2); else TIDE_VERIFY(bf16_t, 1); }
-    else { if (u == 4) TIDE_VERIFY(float, 4); else if (u == 2) TIDE_VERIFY(float, 2); else TIDE_VERIFY(float, 1); }
-#undef TIDE_VERIFY
+    if (!exact) hipLaunchKernelGGL(verify_rough_stats_kernel<T>, grid, block, 0, s, a, (int)parts, u * kStep, stats);
+    else if (u == 4) hipLaunchKernelGGL((verify_stats_kernel<T, 4>), grid, block, 0, s, a, (int)parts, stats);
+    else if (u == 2) hipLaunchKernelGGL((verify_stats_kernel<T, 2>), grid, block, 0, s, a, (int)parts, stats);
+    else hipLaunchKernelGGL((verify_stats_kernel<T, 1>), grid, block, 0, s, a, (int)parts, stats);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  // enough blocks for the chip, and no part below one step
-  const int64_t steps = parts_of(a.V, 1), wanted = std::min<int64_t>({steps, kMaxPicks, std::max<int64_t>(1, 1024 / a.requests)});
-  const int64_t span = (steps + wanted - 1) / wanted * kStep;
-  const int picks = (int)((a.V + span - 1) / span);
-  ProfScope ps("verify_pick", 0, 2.0 * (double)a.requests * a.V * dtype_size(dtype), s);
-  const dim3 grid((unsigned)((int64_t)a.requests * picks)), block(256);
-  if (dtype == kBF16) hipLaunchKernelGGL(verify_pick_kernel<bf16_t>, grid, block, 0, s, a, (int)parts, picks, span, stats, weights, tickets);
-  else hipLaunchKernelGGL(verify_pick_kernel<float>, grid, block, 0, s, a, (int)parts, picks, span, stats, weights, tickets);
+  // 4096 blocks (a full batch of 256 x 128256: 200 us; 2048: 211, 8192: 203, 16384: 216), and no part below one step; of each block's four waves every one has whole units
+  const int per = (int)((a.V + 512 * kMaxUnits - 1) / (512 * kMaxUnits));
+  const int64_t group = (int64_t)per * kStep, groups = (a.V + group - 1) / group;
+  const int64_t wanted = std::min<int64_t>({groups, kMaxPicks, std::max<int64_t>(1, 4096 / a.requests)});
+  const int64_t span = (groups + wanted - 1) / wanted * group;
+  const int picks = (int)((a.V + span - 1) / span), pieces = (int)((a.V + (int64_t)per * 512 - 1) / ((int64_t)per * 512));
+  const dim3 each((unsigned)a.requests), all((unsigned)((int64_t)a.requests * picks));
+  const double row = (double)a.requests * a.V * sizeof(T) * (a.draft ? 2 : 1);
+  {
+    ProfScope ps("verify_decide", 0, 0, s);
+    hipLaunchKernelGGL(verify_decide_kernel<T>, each, dim3(512), 0, s, a, (int)parts, picks, exact, stats, sums, draws);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  if (!exact) {
+    ProfScope ps("verify_sums", 0, row, s);
+    hipLaunchKernelGGL(verify_sums_kernel<T>, all, dim3(256), 0, s, a, picks, span, draws, sums);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  {
+    ProfScope ps("verify_weights", 0, row, s);
+    hipLaunchKernelGGL(verify_weights_kernel<T>, all, dim3(256), 0, s, a, picks, span, per, draws, sums, weights);
+    if (const hipError_t e = hipGetLastError()) return e;
+  }
+  ProfScope ps("verify_pick", 0, 0, s);
+  hipLaunchKernelGGL(verify_pick_kernel<T>, each, dim3(64), 0, s, a, picks, pieces, per, draws, sums, weights);
   return hipGetLastError();
 }
+
+hipError_t launch_verify(const VerifyArgs& a, int dtype, hipStream_t s) { return dtype == kBF16 ? verify<bf16_t>(a, s) : verify<float>(a, s); }
 
 }  // namespace tide
