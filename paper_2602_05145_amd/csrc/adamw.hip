@@ -5,15 +5,18 @@
 #include "kernels.h"
 #include "loose.h"
 #include "prof.h"
+#include "row_stats.h"
 
 namespace tide {
 namespace {
 
-constexpr int kPerThread = 8;                       // consecutive elements
+constexpr int kWide = 4;                            // consecutive elements of a thread: a wave's accesses are one piece of memory each
+constexpr int kPerThread = 8;                       // in two lots
 constexpr int kThreads = 256;
 constexpr int kPerBlock = kPerThread * kThreads;    // 2048 elements of one tensor
 constexpr int kScaled = 256;                        // elements that share a scale: 32 lanes
 constexpr int kPerLaunch = 44;                      // tensors whose table fits the 4 KB of a launch's arguments
+constexpr double kLastCache = 288 << 20;            // bytes from which on nothing is left there for the next call
 constexpr float kTop = 448.f;                       // the largest e4m3 number
 
 struct Entry {
@@ -43,55 +46,90 @@ __host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, int64_t t) 
   return mix(mix(seed ^ (uint32_t)t) + (uint32_t)((uint64_t)t >> 32));
 }
 
-__device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int count) {
-  if (count >= 8) return LDX(u32x2_of_bytes, p);
-  u32x2 c = {0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < count) c[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
-  return c;
+// Four consecutive elements of an array, aligned as one is.  WHOLE: all of them are there; else the first `count`.  ONCE: past the caches.
+template <bool ONCE, typename V> __device__ __forceinline__ auto fetch(const void* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int count, const u32x2& c) {
-  if (count >= 8) { STX(u32x2_of_bytes, p, c); return; }
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < count) p[j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+template <bool ONCE, typename V, typename X> __device__ __forceinline__ void put(void* p, const X& x) {
+  if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = x;
 }
-// e4m3 codes times their scale; every code is exact in fp32
-__device__ __forceinline__ void decode(const u32x2& c, float scale, float (&x)[8]) {
+template <bool WHOLE, bool ONCE>
+struct Four {
+  static __device__ __forceinline__ void load(const float* p, int count, float (&x)[4]) {
+    if constexpr (WHOLE) {
+      const f32x4 a = fetch<ONCE, f32x4_of_floats>(p);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c[h], true);
-    x[4 * h] = lo[0] * scale, x[4 * h + 1] = lo[1] * scale, x[4 * h + 2] = hi[0] * scale, x[4 * h + 3] = hi[1] * scale;
+      for (int j = 0; j < 4; ++j) x[j] = a[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = j < count ? p[j] : 0.f;
+    }
   }
-}
-__device__ __forceinline__ float max_of_32(float v) {   // over the 32 lanes that hold a block
+  static __device__ __forceinline__ void load(const bf16_t* p, int count, float (&x)[4]) {
+    if constexpr (WHOLE) {
+      const u32x2 a = fetch<ONCE, u32x2_of_halves>(p);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+      for (int j = 0; j < 2; ++j) x[2 * j] = __uint_as_float(a[j] << 16), x[2 * j + 1] = __uint_as_float(a[j] & 0xFFFF0000u);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = j < count ? bf2f(p[j]) : 0.f;
+    }
+  }
+  static __device__ __forceinline__ uint32_t load(const uint8_t* p, int count) {
+    if constexpr (WHOLE) return fetch<ONCE, u32_of_bytes>(p);
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < count) c |= (uint32_t)p[j] << (8 * j);
+    return c;
+  }
+  static __device__ __forceinline__ void store(float* p, int count, const float (&x)[4]) {
+    if constexpr (WHOLE) return put<ONCE, f32x4_of_floats>(p, f32x4{x[0], x[1], x[2], x[3]});
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < count) p[j] = x[j];
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, int count, const float (&x)[4]) {
+    if constexpr (WHOLE) return put<ONCE, u32x2_of_halves>(p, u32x2{f2bf2(x[0], x[1]), f2bf2(x[2], x[3])});
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < count) p[j] = f2bf(x[j]);
+  }
+  static __device__ __forceinline__ void store(uint8_t* p, int count, uint32_t c) {
+    if constexpr (WHOLE) return put<ONCE, u32_of_bytes>(p, c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < count) p[j] = (uint8_t)(c >> (8 * j));
+  }
+};
+// e4m3 codes times their scale; every code is exact in fp32
+__device__ __forceinline__ void decode(uint32_t c, float scale, float (&x)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+  x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
 }
 
-// The codes of eight of a block's numbers.  x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
+// The codes of four of a block's numbers, of which a wave holds all.  x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
 // often as it lies beyond the lower: `coin` holds 16 random bits for each.  (To the nearest, a second moment would stand still: a step moves it by up to
 // 1 - beta2 of itself, and the codes lie 6 to 12 % apart.)  Numbers that are not finite become NaN and leave the others alone.
-__device__ __forceinline__ u32x2 encode(const float (&x)[8], const uint32_t (&coin)[8], bool upper, float& scale) {
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&coin)[4], bool upper, float& scale) {
   float top = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]) < INFINITY ? fabsf(x[j]) : 0.f);
-  top = max_of_32(top);
+  for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(x[j]) < INFINITY ? fabsf(x[j]) : 0.f);
+  top = fast_max(top);
   if (!(top >= 0x1p-100f)) top = 0.f;   // (1 / top has to be a number)
   const float factor = top > 0.f ? (1.f / top) * kTop : 0.f;   // (what this rounds moves the largest by a few of the 2^20 that `coin` covers)
   scale = top * (1.f / kTop);
-  u32x2 c = {0, 0};
+  uint32_t c = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 4; ++j) {
     const float y = fminf(fabsf(x[j]) * factor, kTop);
     // below the smallest normal number, 2^-6, the codes are 2^-9 apart as they are up to 2^-5: one more in front makes them alike.  20 bits go.
     const bool low = y < 0x1p-6f;
     const uint32_t bits = __float_as_uint(low ? y + 0x1p-6f : y) + ((upper ? coin[j] >> 16 : coin[j] & 0xFFFFu) << 4) + 8;
     const bool fine = fabsf(x[j]) < INFINITY;
-    const uint32_t code = fine ? ((bits >> 20) - (low ? 968 : 960)) | (x[j] < 0.f ? 0x80u : 0u) : 0x7Fu;
-    c[j / 4] |= code << (8 * (j % 4));
+    c |= (fine ? ((bits >> 20) - (low ? 968 : 960)) | (x[j] < 0.f ? 0x80u : 0u) : 0x7Fu) << (8 * j);
   }
   return c;
 }
@@ -106,66 +144,105 @@ __device__ __forceinline__ void update(const Rate& r, float g, float& m, float& 
   w = w * r.decay - r.lr * (m * r.inv_bc1) / (root * r.inv_sqrt_bc2 + r.eps);
 }
 
-// Block b works on 2048 elements of the tensor its index falls in, a thread on 8 consecutive ones.
+struct Step { Rate r; const float* grad_scale; uint32_t key; };
+
+// 2048 elements of one tensor from element `base` on, in lots of 1024: a wave has one block of 256 of each.  WHOLE: all are there, and every load is under way before the first
+// is waited for.
+template <typename P, typename G, bool EIGHT, bool ONCE, bool WHOLE>
+__device__ __forceinline__ void work(const Entry& t, const Step& s, int64_t base) {
+#pragma clang fp contract(off)
+  constexpr int N = kPerThread / kWide;
+  constexpr bool BF16 = sizeof(P) == 2;
+  using X = Four<WHOLE, ONCE>;
+  float* weights = BF16 ? t.master : (float*)t.param;
+  float g[N][4], w[N][4], m[N][4], v[N][4], root[4], sm[N], sv[N];
+  uint32_t cm[N], cv[N];
+  int64_t i[N];
+  int count[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    i[k] = base + k * (kThreads * kWide) + threadIdx.x * kWide;
+    count[k] = WHOLE ? kWide : (int)min(max(t.n - i[k], (int64_t)0), (int64_t)kWide);
+    X::load((const G*)t.grad + i[k], count[k], g[k]);
+    X::load(weights + i[k], count[k], w[k]);
+    if constexpr (EIGHT) {
+      cm[k] = X::load((const uint8_t*)t.m + i[k], count[k]);
+      cv[k] = X::load((const uint8_t*)t.v + i[k], count[k]);
+      const int64_t block = (WHOLE ? i[k] : min(i[k], t.n - 1)) / kScaled;
+      sm[k] = t.m_scale[block], sv[k] = t.v_scale[block];
+    } else {
+      X::load((const float*)t.m + i[k], count[k], m[k]);
+      X::load((const float*)t.v + i[k], count[k], v[k]);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if constexpr (EIGHT) {
+      decode(cm[k], sm[k], m[k]);
+      decode(cv[k], sv[k], v[k]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[k][j] = v[k][j] * v[k][j];
+    }
+    if (s.grad_scale) {
+      const float f = *s.grad_scale;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[k][j] *= f;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) update(s.r, g[k][j], m[k][j], v[k][j], root[j], w[k][j]);
+    X::store(weights + i[k], count[k], w[k]);
+    if constexpr (BF16) X::store((bf16_t*)t.param + i[k], count[k], w[k]);
+    if constexpr (EIGHT) {
+      const uint32_t key = s.key + (uint32_t)i[k] + (uint32_t)((uint64_t)i[k] >> 32) * 0x9E3779B9u;
+      uint32_t coin[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        coin[j] = mix(key + j);   // (i is a multiple of four: its upper half is the same for all)
+        if (!WHOLE && j >= count[k]) m[k][j] = root[j] = 0.f;
+      }
+      X::store((uint8_t*)t.m + i[k], count[k], encode(m[k], coin, false, sm[k]));
+      X::store((uint8_t*)t.v + i[k], count[k], encode(root, coin, true, sv[k]));
+      if (count[k] > 0 && threadIdx.x % (kScaled / kWide) == 0) t.m_scale[i[k] / kScaled] = sm[k], t.v_scale[i[k] / kScaled] = sv[k];
+    } else {
+      X::store((float*)t.m + i[k], count[k], m[k]);
+      X::store((float*)t.v + i[k], count[k], v[k]);
+    }
+  }
+}
+template <typename P, typename G, bool EIGHT, bool ONCE>
+__device__ __forceinline__ void work(const Entry& t, const Step& s, int64_t base) {
+  if (base + kPerBlock <= t.n) work<P, G, EIGHT, ONCE, true>(t, s, base);
+  else work<P, G, EIGHT, false, false>(t, s, base);
+}
+
+// Block b works on 2048 elements of the tensor its index falls in.  Bound by memory.  Past the caches (both ways) where a launch moves more than they hold: the small draft of
+// 216M weights, 32 bits, 702 -> 674 us (5.6 TB/s), the large one of 794M, 8 bits, 2750 -> 2555; 2M weights, which the last cache holds, 10.2 -> 11.2.
+template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const Table a) {
 #pragma clang fp contract(off)
   const int lane = threadIdx.x & 63;
   const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < kPerLaunch && a.first[min(lane, kPerLaunch - 1)] <= blockIdx.x)) - 1);
   const Entry& t = a.t[at];
-  const int64_t i = (int64_t)(blockIdx.x - a.first[at]) * kPerBlock + threadIdx.x * kPerThread;
-  const int count = (int)min(max(t.n - i, (int64_t)0), (int64_t)kPerThread);
-  if (!(t.flags & kEightBits) && count == 0) return;   // (lanes of a shared scale stay)
+  const int64_t base = (int64_t)(blockIdx.x - a.first[at]) * kPerBlock;
   const bool dyn = a.schedule != nullptr;
-  Rate r;
-  r.lr = dyn ? a.schedule->lr : a.lr;
-  r.inv_bc1 = dyn ? a.schedule->inv_bc1 : a.inv_bc1;
-  r.inv_sqrt_bc2 = dyn ? a.schedule->inv_sqrt_bc2 : a.inv_sqrt_bc2;
-  r.decay = 1.f - r.lr * t.decay;
-  r.beta1 = a.beta1, r.beta2 = a.beta2, r.rest1 = 1.f - a.beta1, r.rest2 = 1.f - a.beta2, r.eps = a.eps;
-  float g[8], w[8], m[8], v[8], root[8];
-  if (count > 0 && (t.flags & kGradBf16)) load_some((const bf16_t*)t.grad + i, count, g);
-  else load_some((const float*)t.grad + i, count, g);
-  float* weights = (t.flags & kParamBf16) ? t.master : (float*)t.param;
-  load_some(weights + i, count, w);
-  if (t.flags & kEightBits) {
-    const u32x2 cm = load_codes((const uint8_t*)t.m + i, count), cv = load_codes((const uint8_t*)t.v + i, count);
-    const int64_t block = min(i, t.n - 1) / kScaled;
-    decode(cm, t.m_scale[block], m);
-    decode(cv, t.v_scale[block], v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * v[j];
-  } else {
-    load_some((const float*)t.m + i, count, m);
-    load_some((const float*)t.v + i, count, v);
+  Step s;
+  s.r.lr = dyn ? a.schedule->lr : a.lr;
+  s.r.inv_bc1 = dyn ? a.schedule->inv_bc1 : a.inv_bc1;
+  s.r.inv_sqrt_bc2 = dyn ? a.schedule->inv_sqrt_bc2 : a.inv_sqrt_bc2;
+  s.r.decay = 1.f - s.r.lr * t.decay;
+  s.r.beta1 = a.beta1, s.r.beta2 = a.beta2, s.r.rest1 = 1.f - a.beta1, s.r.rest2 = 1.f - a.beta2, s.r.eps = a.eps;
+  s.grad_scale = a.grad_scale;
+  s.key = mix((dyn ? a.schedule->key : a.key) + t.index);
+  switch (t.flags) {
+    case 0: work<float, float, false, ONCE>(t, s, base); break;
+    case kGradBf16: work<float, bf16_t, false, ONCE>(t, s, base); break;
+    case kParamBf16: work<bf16_t, float, false, ONCE>(t, s, base); break;
+    case kParamBf16 | kGradBf16: work<bf16_t, bf16_t, false, ONCE>(t, s, base); break;
+    case kEightBits: work<float, float, true, ONCE>(t, s, base); break;
+    case kEightBits | kGradBf16: work<float, bf16_t, true, ONCE>(t, s, base); break;
+    case kEightBits | kParamBf16: work<bf16_t, float, true, ONCE>(t, s, base); break;
+    default: work<bf16_t, bf16_t, true, ONCE>(t, s, base);
   }
-  if (a.grad_scale) {
-    const float s = *a.grad_scale;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] *= s;
-  }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) update(r, g[j], m[j], v[j], root[j], w[j]);
-  store_some(weights + i, count, w);
-  if (t.flags & kParamBf16) store_some((bf16_t*)t.param + i, count, w);
-  if (!(t.flags & kEightBits)) {
-    store_some((float*)t.m + i, count, m);
-    store_some((float*)t.v + i, count, v);
-    return;
-  }
-  const uint32_t key = mix((dyn ? a.schedule->key : a.key) + t.index) + (uint32_t)i + (uint32_t)((uint64_t)i >> 32) * 0x9E3779B9u;
-  uint32_t coin[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) coin[j] = mix(key + j);   // (i is a multiple of 8: its upper half is the same for all)
-  if (count < 8) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j >= count) m[j] = root[j] = 0.f;
-  }
-  float sm, sv;
-  const u32x2 cm = encode(m, coin, false, sm), cv = encode(root, coin, true, sv);
-  store_codes((uint8_t*)t.m + i, count, cm);
-  store_codes((uint8_t*)t.v + i, count, cv);
-  if (count > 0 && (lane & 31) == 0) t.m_scale[i / kScaled] = sm, t.v_scale[i / kScaled] = sv;
 }
 
 __global__ void adamw_schedule_kernel(const float* __restrict__ lr, int64_t* __restrict__ step, float beta1, float beta2, uint32_t seed, AdamwSchedule* __restrict__ out) {
@@ -209,7 +286,8 @@ hipError_t launch_adamw_list(const AdamwListArgs& a, hipStream_t s) {
     }
     if (n == 0) break;
     ProfScope ps("adamw_list", 0, bytes, s);
-    hipLaunchKernelGGL(adamw_list_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, d);
+    if (bytes > kLastCache) hipLaunchKernelGGL(adamw_list_kernel<true>, dim3((unsigned)blocks), dim3(kThreads), 0, s, d);
+    else hipLaunchKernelGGL(adamw_list_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, d);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;

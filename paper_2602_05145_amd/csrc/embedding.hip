@@ -15,209 +15,269 @@ constexpr int kIdBits = 21;       // ids are below 2^21, and a chunk's place tak
 constexpr uint32_t kNone = (1u << kIdBits) - 1;   // id of a row without a token; no vocabulary reaches it
 static_assert(kIdBits + 11 == 32 && kChunk == 1 << 11);
 
-// One wave copies kCols columns of a row.
-template <typename T>
+// Eight columns of a row for each lane.  The last of a row that is no multiple of eight wide are the row's last eight, of which a lane writes those that no other does (`skip`); lanes
+// behind them write nothing.  So every lane loads eight, and no load waits for a branch.  TINY: rows below eight columns, one by one.
+template <bool TINY>
+struct Lane {
+  int at, skip;
+  __device__ __forceinline__ Lane(int c, int d) : at(TINY ? 0 : min(c, d - 8)), skip(TINY ? (c > 0 ? 8 : 8 - d) : min(c - at, 8)) {}
+  template <typename T> __device__ __forceinline__ void load(Loose8<T>& x, const T* row) const {
+    if constexpr (TINY) x.load_some(row, 8 - skip);
+    else x.load(row + at);
+  }
+  template <typename T> __device__ __forceinline__ void store(T* row, const float (&x)[8]) const {
+    if (!TINY && skip == 0) return store_loose8(row + at, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (TINY ? j < 8 - skip : j >= skip) stf(row, at + j, x[j]);
+  }
+};
+template <typename T> __device__ __forceinline__ void add8(const Loose8<T>& raw, float (&sum)[8]) {
+  float x[8];
+  raw.get(x);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[j] += x[j];
+}
+
+// One wave copies G * kCols columns of a row, all of its loads under way together.
+template <typename T, int G, bool TINY>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(int64_t rows, int vocab, int d, int tiles, const int32_t* __restrict__ ids, const T* __restrict__ table,
                                                         float scale, T* __restrict__ out) {
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t row = w / tiles;
   if (row >= rows) return;
-  const int c = (int)(w % tiles) * kCols + (threadIdx.x & 63) * 8, count = min(8, d - c);
-  if (count <= 0) return;
-  const int id = ids[row];
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (id >= 0 && id < vocab) {
-    load_some(table + (size_t)id * d + c, count, x);
+  const int c = (int)(w % tiles) * (G * kCols) + (threadIdx.x & 63) * 8;
+  const int id = __builtin_amdgcn_readfirstlane(ids[row]);
+  const bool some = id >= 0 && id < vocab;
+  const T* from = table + (size_t)(some ? id : 0) * d;
+  Loose8<T> raw[G];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= scale;
+  for (int g = 0; g < G; ++g) Lane<TINY>(c + g * kCols, d).load(raw[g], from);
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    float x[8];
+    raw[g].get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = some ? x[j] * scale : 0.f;
+    Lane<TINY>(c + g * kCols, d).store(out + (size_t)row * d, x);
   }
-  store_some(out + (size_t)row * d + c, count, x);
 }
 
-// The first `chunks` blocks sort kChunk ids each, with their places, by id and then by place; the others clear the gradient, where it is written and not
-// added to, while they do.
-__global__ __launch_bounds__(1024) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
-                                                          int32_t* __restrict__ pos, uint32_t* __restrict__ clear, size_t head, size_t words, int tail) {
+// Bitonic order of kChunk keys, eight consecutive ones a thread: distances below 8 in a thread's registers, up to 256 between the lanes of a wave, 512 and 1024 through LDS.
+__device__ __forceinline__ void sort_chunk(uint32_t (&key)[8], uint32_t* lds) {
+  const int t = threadIdx.x;
+  auto keep = [&](int i, uint32_t other, int j, int k) {   // of a pair at distance j, the lower place keeps the smaller where its run of k ascends
+    const int e = t * 8 + i;
+    const bool smaller = ((e & j) == 0) == ((e & k) == 0);
+    key[i] = smaller ? min(key[i], other) : max(key[i], other);
+  };
+#pragma unroll
+  for (int k = 2; k <= kChunk; k *= 2) {
+#pragma unroll
+    for (int j = kChunk / 2; j > 0; j /= 2) {
+      if (j >= k) continue;
+      if (j >= 512) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[i * 256 + t] = key[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) keep(i, lds[i * 256 + (t ^ (j / 8))], j, k);
+      } else if (j >= 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) keep(i, __shfl_xor(key[i], j / 8, 64), j, k);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((i & j) == 0) {
+            const uint32_t a = key[i], b = key[i | j];
+            const bool up = (((t * 8 + i) & k) == 0);
+            key[i] = up ? min(a, b) : max(a, b);
+            key[i | j] = up ? max(a, b) : min(a, b);
+          }
+      }
+    }
+  }
+}
+
+// The first `chunks` blocks sort kChunk ids each, with their places, by id and then by place (no two keys are alike: there is one order); the others clear the gradient, where it
+// is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.
+__global__ __launch_bounds__(256) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
+                                                         int32_t* __restrict__ pos, uint8_t* __restrict__ clear, size_t head, size_t words, int tail) {
   if (blockIdx.x >= chunks) {
-    // `head` bytes up to a multiple of 16, then 16-byte words, then `tail` bytes
-    uint8_t* bytes = reinterpret_cast<uint8_t*>(clear);
-    const size_t at = (size_t)(blockIdx.x - chunks) * 1024 + threadIdx.x, step = (size_t)(gridDim.x - chunks) * 1024;
-    u32x4* body = reinterpret_cast<u32x4*>(bytes + head);
+    const size_t at = (size_t)(blockIdx.x - chunks) * 256 + threadIdx.x, step = (size_t)(gridDim.x - chunks) * 256;
+    u32x4* body = reinterpret_cast<u32x4*>(clear + head);
     for (size_t i = at; i < words; i += step) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, body + i);
-    if (at < head) bytes[at] = 0;
-    if (at < (size_t)tail) bytes[head + words * 16 + at] = 0;
+    if (at < head) clear[at] = 0;
+    if (at < (size_t)tail) clear[head + words * 16 + at] = 0;
     return;
   }
-  __shared__ uint32_t key[kChunk];
+  __shared__ uint32_t lds[kChunk];
   const int64_t base = (int64_t)blockIdx.x * kChunk;
-  for (int i = threadIdx.x; i < kChunk; i += 1024) {
-    const int64_t row = base + i;
-    const int id = row < rows ? ids[row] : -1;
-    key[i] = id >= 0 && id < vocab ? (uint32_t)id << 11 | (uint32_t)i : kNone << 11 | (uint32_t)i;
+  uint32_t key[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = threadIdx.x * 8 + i;
+    const int id = base + at < rows ? ids[base + at] : -1;
+    key[i] = (id >= 0 && id < vocab ? (uint32_t)id : kNone) << 11 | (uint32_t)at;
   }
-  // bitonic: no two keys are alike, so that the order is the one order there is
-  for (int k = 2; k <= kChunk; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
-      __syncthreads();
-      const int i = 2 * threadIdx.x - (threadIdx.x & (j - 1)), o = i + j;
-      const uint32_t a = key[i], b = key[o];
-      if ((a > b) == ((i & k) == 0)) key[i] = b, key[o] = a;
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < kChunk; i += 1024) sid[base + i] = key[i] >> 11, pos[base + i] = (int32_t)(base + (key[i] & (kChunk - 1)));
+  sort_chunk(key, lds);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t at = base + threadIdx.x * 8 + i;
+    sid[at] = key[i] >> 11, pos[at] = (int32_t)(base + (key[i] & (kChunk - 1)));
+  }
 }
 
-// Joins kWays sorted runs of `run` each: a row's place is its own and, of every other run, how many come before it (equal ids: those of earlier runs).
-__global__ __launch_bounds__(256) void embed_merge_kernel(int64_t total, int64_t run, const uint32_t* __restrict__ sid, const int32_t* __restrict__ pos,
-                                                          uint32_t* __restrict__ sid_out, int32_t* __restrict__ pos_out) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= total) return;
+// Joins kWays sorted runs of `run` each: a row's place is its own and, of every other run, how many come before it (equal ids: those of earlier runs).  Four threads a row, each
+// for a quarter of the runs.  IN_LDS: the ids that a block's rows are joined with are copied there first.
+template <bool IN_LDS>
+__global__ __launch_bounds__(1024) void embed_merge_kernel(int64_t total, int64_t run, const uint32_t* __restrict__ sid, const int32_t* __restrict__ pos,
+                                                           uint32_t* __restrict__ sid_out, int32_t* __restrict__ pos_out) {
+  extern __shared__ uint32_t lds[];
+  constexpr int kMine = kWays / 4;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x / 4;   // (total is a multiple of 256)
   const int64_t group = e / (run * kWays) * (run * kWays);
-  const int own = (int)((e - group) / run);
+  const int own = (int)((e - group) / run), here = (int)min(run * kWays, total - group), first_run = (threadIdx.x & 3) * kMine;
   const uint32_t id = sid[e];
-  int64_t found[kWays];
+  const int32_t place = pos[e];
+  const uint32_t* of = sid + group;
+  if constexpr (IN_LDS) {
+    constexpr int kCopies = kWays * kChunk / 4096;
+    u32x4 x[kCopies];
 #pragma unroll
-  for (int s = 0; s < kWays; ++s) found[s] = 0;
-  for (int64_t half = run; half > 0; half /= 2)   // (a power of two)
+    for (int k = 0; k < kCopies; ++k) x[k] = *reinterpret_cast<const u32x4*>(of + min(k * 4096 + (int)threadIdx.x * 4, here - 4));   // all under way together
 #pragma unroll
-    for (int s = 0; s < kWays; ++s) {
-      const int64_t first = group + s * run, length = min(run, total - first), next = found[s] + half;
-      if (s == own || next > length) continue;   // (the last run may be short or missing)
-      const uint32_t other = sid[first + next - 1];
-      if (s < own ? other <= id : other < id) found[s] = next;
+    for (int k = 0; k < kCopies; ++k)
+      if (k * 4096 + (int)threadIdx.x * 4 < here) *reinterpret_cast<u32x4*>(lds + k * 4096 + threadIdx.x * 4) = x[k];
+    __syncthreads();
+    of = lds;
+  }
+  int found[kMine];
+#pragma unroll
+  for (int s = 0; s < kMine; ++s) found[s] = 0;
+  for (int half = (int)run; half > 0; half /= 2)   // (a power of two)
+#pragma unroll
+    for (int s = 0; s < kMine; ++s) {
+      const int r = first_run + s, first = r * (int)run, length = min((int)run, here - first), next = found[s] + half;
+      const bool inside = r != own && next <= length;   // (the last run may be short or missing)
+      const uint32_t other = of[inside ? first + next - 1 : 0];
+      if (inside && other < id + (r < own)) found[s] = next;
     }
-  int64_t to = e - own * run;
+  int before = 0;
 #pragma unroll
-  for (int s = 0; s < kWays; ++s) to += found[s];
-  sid_out[to] = id, pos_out[to] = pos[e];
-}
-
-template <typename T> struct Row8;   // eight elements as loaded
-template <> struct Row8<bf16_t> {
-  u32x4 a;
-  __device__ __forceinline__ void load(const bf16_t* p, int count) {
-    if (count >= 8) { a = LDX(u32x4_of_halves, p); return; }
-    a = u32x4{0, 0, 0, 0};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < count) a[j / 2] |= (uint32_t)p[j] << (16 * (j % 2));
-  }
-  __device__ __forceinline__ void add(float (&x)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[2 * j] += __uint_as_float(a[j] << 16), x[2 * j + 1] += __uint_as_float(a[j] & 0xFFFF0000u);
-  }
-};
-template <> struct Row8<float> {
-  f32x4 a, b;
-  __device__ __forceinline__ void load(const float* p, int count) {
-    if (count >= 8) { a = LDX(f32x4_of_floats, p), b = LDX(f32x4_of_floats, p + 4); return; }
-    a = b = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (j < count) a[j] = p[j];
-      if (4 + j < count) b[j] = p[4 + j];
-    }
-  }
-  __device__ __forceinline__ void add(float (&x)[8]) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] += a[j], x[4 + j] += b[j];
-  }
-};
-
-template <typename G>
-__device__ __forceinline__ void finish(G* to, int count, float scale, bool accumulate, const float (&sum)[8]) {
-  float x[8], old[8];
-  if (accumulate) load_some(to, count, old);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = accumulate ? fmaf(scale, sum[j], old[j]) : scale * sum[j];
-  store_some(to, count, x);
+  for (int s = 0; s < kMine; ++s) before += found[s];
+  before += __shfl_xor(before, 1, 64);
+  before += __shfl_xor(before, 2, 64);
+  const int64_t to = e - own * run + before;
+  if ((threadIdx.x & 3) == 0) sid_out[to] = id;
+  if ((threadIdx.x & 3) == 1) pos_out[to] = place;
 }
 
 // A wave adds up kCols columns of `piece` rows that follow each other in the order of their tokens.  A token whose rows all lie in the piece is done;
 // of one that goes on in front of or behind it, what lies here is left as a part: parts[2 p] for the first token, parts[2 p + 1] for the last (the first, where there is but
-// one and it goes on in front).
-template <typename T, typename G>
+// one and it goes on in front).  What is added to is requested with the rows, not when their sum is there.  Bound by memory: 32768 rows x 4096 (bf16, to fp32)
+// of as many tokens at 5.3 TB/s, of 1000 tokens (rows in the last cache) at 6.2.
+template <typename T, typename G, bool ADD, bool TINY>
 __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece, int d, int tiles, const uint32_t* __restrict__ sid, const int32_t* __restrict__ pos,
-                                                        const T* __restrict__ dy, float scale, G* __restrict__ dtable, int accumulate, float* __restrict__ parts) {
-  constexpr int U = 8;
+                                                        const T* __restrict__ dy, float scale, G* __restrict__ dtable, float* __restrict__ parts) {
+  constexpr int U = ADD ? 4 : 8;
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t p = w / tiles, first = p * piece;
   if (first >= total) return;
   const int lane = threadIdx.x & 63;
-  const int c = (int)(w % tiles) * kCols + lane * 8, count = min(8, d - c);
+  const Lane<TINY> own((int)(w % tiles) * kCols + lane * 8, d);
   const int64_t mine = first + min(lane, piece - 1);   // (total is a multiple of every piece)
   const uint32_t my_id = sid[mine];
   const int my_row = pos[mine];
   const uint32_t before = first > 0 ? sid[first - 1] : kNone, behind = first + piece < total ? sid[first + piece] : kNone;
-  uint32_t id = __builtin_amdgcn_readlane(my_id, 0);
-  if (id == kNone) return;
-  bool open = before == id;     // whether the token at hand goes on in front of the piece
+  if (__builtin_amdgcn_readlane(my_id, 0) == kNone) return;
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto leave = [&](bool goes_on) {
-    if (count > 0) {
-      if (open || goes_on) store_some(parts + (size_t)(2 * p + (open ? 0 : 1)) * d + c, count, sum);
-      else finish(dtable + (size_t)id * d + c, count, scale, accumulate, sum);
-    }
-    open = false;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-  };
   for (int k0 = 0; k0 < piece; k0 += U) {
-    Row8<T> raw[U];
+    Loose8<T> raw[U];
+    Loose8<G> old[ADD ? U : 1];
+    uint32_t id[U + 1];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = __builtin_amdgcn_readlane(my_id, k0 + u);
+    id[U] = k0 + U < piece ? __builtin_amdgcn_readlane(my_id, min(k0 + U, 63)) : behind;
+    // (a row without a token, and a sum that is not final, ask for the first row of either: no load stands behind a branch)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t at = __builtin_amdgcn_readlane(my_id, k0 + u);
-      const T* row = dy + (size_t)__builtin_amdgcn_readlane(my_row, k0 + u) * d + c;
-      if (at == kNone) continue;   // (uniform)
-      raw[u].load(row, count);
+      own.load(raw[u], dy + (id[u] == kNone ? (size_t)0 : (size_t)__builtin_amdgcn_readlane(my_row, k0 + u) * d));
+      if constexpr (ADD) own.load(old[u], dtable + (id[u] != id[u + 1] && id[u] != before ? (size_t)id[u] * d : (size_t)0));
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const uint32_t at = __builtin_amdgcn_readlane(my_id, k0 + u);
-      if (at != id) {
-        leave(false);
-        id = at;
+      if (id[u] == kNone) return;   // what follows has no token either
+      add8(raw[u], sum);
+      const bool ends = id[u] != id[u + 1];
+      if (!ends && k0 + u + 1 < piece) continue;
+      if (id[u] == before || !ends) {
+        own.store(parts + (size_t)(2 * p + (id[u] == before ? 0 : 1)) * d, sum);
+      } else {
+        float x[8];
+        if constexpr (ADD) {
+          old[u].get(x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
+        }
+        own.store(dtable + (size_t)id[u] * d, x);
       }
-      if (at == kNone) return;   // what follows has no token either
-      raw[u].add(sum);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] = 0.f;
     }
   }
-  leave(behind == id);
 }
 
 // Adds up the parts of a token that reaches over pieces, from the piece it begins in.
-template <typename G>
+template <typename G, bool ADD, bool TINY>
 __global__ __launch_bounds__(256) void embed_join_kernel(int64_t total, int piece, int d, int tiles, const uint32_t* __restrict__ sid, float scale, G* __restrict__ dtable,
-                                                         int accumulate, const float* __restrict__ parts) {
+                                                         const float* __restrict__ parts) {
+  constexpr int U = 8;
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t p = w / tiles, end = (p + 1) * piece;
   if (end >= total) return;   // nothing goes on behind the last one
-  const uint32_t id = sid[end - 1];
-  if (id == kNone || sid[end] != id) return;
-  if (p > 0 && sid[p * piece - 1] == id) return;   // begins before
-  // how many pieces it reaches into: the first place behind it, by steps that double and then halve
-  int64_t lo = end, step = 1;   // sid[lo] == id
-  while (lo + step < total && sid[lo + step] == id) lo += step, step *= 2;
-  for (; step > 0; step /= 2)
-    if (lo + step < total && sid[lo + step] == id) lo += step;
-  const int64_t last = lo / piece;
-  const int c = (int)(w % tiles) * kCols + (threadIdx.x & 63) * 8, count = min(8, d - c);
-  if (count <= 0) return;
-  float sum[8];
-  load_some(parts + (size_t)(2 * p + 1) * d + c, count, sum);
-  for (int64_t q = p + 1; q <= last; q += 4) {
-    float x[4][8];
+  const int lane = threadIdx.x & 63;
+  const uint32_t before = p > 0 ? sid[p * piece - 1] : kNone, id = sid[end - 1];
+  const int64_t reach = end + (int64_t)lane * piece;
+  const uint32_t starts = reach < total ? sid[reach] : kNone;   // what the pieces behind begin with
+  if (id == kNone || id == before) return;                      // begins before
+  unsigned long long goes_on = __ballot(starts == id);
+  if (!(goes_on & 1)) return;
+  const Lane<TINY> own((int)(w % tiles) * kCols + lane * 8, d);
+  float sum[8], x[8];
+  Loose8<G> old;
+  Loose8<float> begun;
+  if constexpr (ADD) own.load(old, dtable + (size_t)id * d);
+  own.load(begun, parts + (size_t)(2 * p + 1) * d);
+  begun.get(sum);
+  for (int64_t q = p + 1;;) {
+    const int n = ~goes_on ? __ffsll(~goes_on) - 1 : 64;   // pieces from q on that the token reaches into
+    for (int k = 0; k < n; k += U) {
+      Loose8<float> raw[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (q + u <= last) load_some(parts + (size_t)(2 * (q + u)) * d + c, count, x[u]);
+      for (int u = 0; u < U; ++u) own.load(raw[u], parts + (size_t)(2 * (q + min(k + u, n - 1))) * d);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (q + u <= last) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += x[u][j];
-      }
+      for (int u = 0; u < U; ++u)
+        if (k + u < n) add8(raw[u], sum);
+    }
+    if (n < 64) break;
+    q += 64;
+    const int64_t next = (q + lane) * piece;
+    goes_on = __ballot((next < total ? sid[next] : kNone) == id);
   }
-  finish(dtable + (size_t)id * d + c, count, scale, accumulate, sum);
+  if constexpr (ADD) {
+    old.get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
+  }
+  own.store(dtable + (size_t)id * d, x);
 }
 
 struct Plan {
@@ -243,18 +303,35 @@ Plan make_plan(int64_t rows, int64_t d) {
   return p;
 }
 
-template <typename T, typename G>
+template <typename T, typename G, bool ADD, bool TINY>
 hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const int32_t* pos, float* parts, hipStream_t s) {
   const unsigned blocks = (unsigned)((p.pieces * p.tiles + 3) / 4);
   {
     ProfScope ps("embed_sum", (double)a.rows * a.d, (double)a.rows * a.d * sizeof(T), s);
-    hipLaunchKernelGGL((embed_sum_kernel<T, G>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable,
-                       a.accumulate, parts);
+    hipLaunchKernelGGL((embed_sum_kernel<T, G, ADD, TINY>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable, parts);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (p.pieces < 2) return hipSuccess;
   ProfScope ps("embed_join", 0, 0, s);
-  hipLaunchKernelGGL((embed_join_kernel<G>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, a.scale, (G*)a.dtable, a.accumulate, parts);
+  hipLaunchKernelGGL((embed_join_kernel<G, ADD, TINY>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, a.scale, (G*)a.dtable, parts);
+  return hipGetLastError();
+}
+
+template <typename T, typename G>
+hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const int32_t* pos, float* parts, hipStream_t s) {
+  if (a.d < 8) return a.accumulate ? sums<T, G, true, true>(a, p, sid, pos, parts, s) : sums<T, G, false, true>(a, p, sid, pos, parts, s);
+  return a.accumulate ? sums<T, G, true, false>(a, p, sid, pos, parts, s) : sums<T, G, false, false>(a, p, sid, pos, parts, s);
+}
+
+template <typename T>
+hipError_t embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, const T* table, float scale, T* out, hipStream_t s) {
+  // few rows: a wave for each 512 columns; many: for each 2048
+  const bool few = rows * ((d + kCols - 1) / kCols) < 16384;
+  const int wide = few ? kCols : 4 * kCols, tiles = (d + wide - 1) / wide;
+  const unsigned blocks = (unsigned)((rows * tiles + 3) / 4);
+  if (d < 8) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, true>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, rows, vocab, d, 1, ids, table, scale, out);
+  else if (few) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, false>), dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, table, scale, out);
+  else hipLaunchKernelGGL((embed_fwd_kernel<T, 4, false>), dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, table, scale, out);
   return hipGetLastError();
 }
 
@@ -262,12 +339,9 @@ hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const
 
 hipError_t launch_embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, const void* table, float scale, void* out, int dtype, hipStream_t s) {
   if (rows <= 0) return hipSuccess;
-  const int tiles = (d + kCols - 1) / kCols;
-  const unsigned blocks = (unsigned)((rows * tiles + 3) / 4);
   ProfScope ps("embed_fwd", 0, 2.0 * (double)rows * d * dtype_size(dtype), s);
-  if (dtype == kBF16) hipLaunchKernelGGL(embed_fwd_kernel<bf16_t>, dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, (const bf16_t*)table, scale, (bf16_t*)out);
-  else hipLaunchKernelGGL(embed_fwd_kernel<float>, dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, (const float*)table, scale, (float*)out);
-  return hipGetLastError();
+  return dtype == kBF16 ? embed_fwd<bf16_t>(rows, vocab, d, ids, (const bf16_t*)table, scale, (bf16_t*)out, s)
+                        : embed_fwd<float>(rows, vocab, d, ids, (const float*)table, scale, (float*)out, s);
 }
 
 size_t embed_bwd_workspace_bytes(int64_t rows, int64_t d) { return make_plan(std::max<int64_t>(rows, 1), d).bytes; }
@@ -279,21 +353,28 @@ hipError_t launch_embed_bwd(const EmbedBwdArgs& a, hipStream_t s) {
   const size_t bytes = a.accumulate ? 0 : (size_t)a.vocab * (size_t)a.d * dtype_size(a.table_dtype);
   const size_t head = std::min(bytes, (16 - ((uintptr_t)a.dtable & 15)) & 15), words = (bytes - head) / 16;
   const int tail = (int)(bytes - head - words * 16);
-  const int clear = bytes ? (int)std::min<size_t>((words + 4095) / 4096 + 1, 2048) : 0;
+  const int clear = bytes ? (int)std::min<size_t>((words + 1023) / 1024 + 1, 8192) : 0;
   uint32_t* sid[2];
   int32_t* pos[2];
   for (int k = 0; k < 2; ++k) sid[k] = (uint32_t*)(ws + p.ids[k]), pos[k] = (int32_t*)(sid[k] + p.total);
   if (chunks + clear == 0) return hipSuccess;
   {
     ProfScope ps("embed_sort", 0, (double)bytes, s);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(chunks + clear), dim3(1024), 0, s, a.rows, a.vocab, chunks, a.ids, sid[0], pos[0], (uint32_t*)a.dtable, head, words, tail);
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(chunks + clear), dim3(256), 0, s, a.rows, a.vocab, chunks, a.ids, sid[0], pos[0], (uint8_t*)a.dtable, head, words, tail);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (a.rows <= 0) return hipSuccess;
   int at = 0;
   for (int64_t run = kChunk; run < p.total; run *= kWays, at ^= 1) {
     ProfScope ps("embed_merge", 0, 0, s);
-    hipLaunchKernelGGL(embed_merge_kernel, dim3((unsigned)(p.total / 256)), dim3(256), 0, s, p.total, run, sid[at], pos[at], sid[at ^ 1], pos[at ^ 1]);
+    const dim3 grid((unsigned)(p.total / 256)), block(1024);
+    if (run == kChunk) {
+      const size_t lds = (size_t)std::min<int64_t>(p.total, kChunk * kWays) * sizeof(uint32_t);
+      if (const hipError_t e = hipFuncSetAttribute((const void*)embed_merge_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, kChunk * kWays * sizeof(uint32_t))) return e;
+      hipLaunchKernelGGL(embed_merge_kernel<true>, grid, block, lds, s, p.total, run, sid[at], pos[at], sid[at ^ 1], pos[at ^ 1]);
+    } else {
+      hipLaunchKernelGGL(embed_merge_kernel<false>, grid, block, 0, s, p.total, run, sid[at], pos[at], sid[at ^ 1], pos[at ^ 1]);
+    }
     if (const hipError_t e = hipGetLastError()) return e;
   }
   float* parts = (float*)(ws + p.parts);

@@ -651,9 +651,9 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a, int
 
 int64_t parts_of(int64_t V, int u) { return (V + (int64_t)u * kStep - 1) / ((int64_t)u * kStep); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// Up to so many columns in all rows the exact sums are made at once, which saves a launch: 5M 20.7 us beside 23.8 with sums in 32 bits first, 10M 25.1 / 24.9, 18M 34.8 / 30.4,
+// Up to so many columns in all rows the exact sums are made at once, which saves a launch: 5M 20.7 us beside 23.8 with sums in 32 bits first, 11M 27.1 / 29.5, 18M 34.8 / 30.4,
 // 295M 304 / 178 (bf16).
-constexpr int64_t kFewColumns = 10 << 20;
+constexpr int64_t kFewColumns = 12 << 20;
 
 }  // namespace
 
@@ -673,7 +673,7 @@ static hipError_t verify(const VerifyArgs& a, hipStream_t s) {
   const bool exact = units * a.V <= kFewColumns;
   // exact: registers hold up to 8192 columns of a block; else a block goes over up to 32768 (16384 and 65536: 1 % slower), less where that leaves CUs idle
   int u = exact ? 4 : 16;
-  while (u > 1 && units * parts_of(a.V, u) < 2048) u /= 2;
+  while (u > 1 && (units * parts_of(a.V, u) < 2048 || (int64_t)u / 2 * kStep >= a.V)) u /= 2;
   const int64_t parts = parts_of(a.V, u);
   {
     ProfScope ps("verify_stats", 4.0 * (double)units * a.V, (double)units * a.V * sizeof(T), s);

@@ -73,10 +73,18 @@ def test_numbers_of_requests_and_drafts(lens):
 
 
 def test_large_batches_take_wider_parts():
-    """Rows enough for parts of 4096 and of 8192 columns."""
-    for requests, vocab in ((60, 20003), (200, 20003)):
-        data = batch([4] * requests, vocab, "bf16", 9, near=0.4)
-        check(*data, vocab, "bf16")
+    """Rows enough for wider parts, for sums in 32 bits first, and for parts of 16384 and 32768 columns; requests without sampling, without a distribution and at
+    temperatures for which 32 bits are no good among them; a draft and none."""
+    for requests, vocab, dtype in ((60, 20003, "bf16"), (200, 20003, "fp32"), (40, 128256, "bf16"), (70, 40001, "bf16")):
+        cu, target, draft, tokens, temperature, uniforms = batch([4] * requests, vocab, dtype, 9, near=0.4)
+        check(cu, target, draft, tokens, temperature, uniforms, vocab, dtype)
+        temperature[::5] = 0.0
+        temperature[1], temperature[6], temperature[7], temperature[8] = 1e-32, 1e32, NAN, -1.0
+        target[5 * 11 + 1, 17], target[5 * 12, vocab - 1], draft[4 * 13 + 2, 8] = NAN, INF, NAN
+        target[5 * 14, :vocab] = -INF
+        target[5 * 16:5 * 18, 5:vocab:2] = -INF
+        check(cu, target, draft, tokens, temperature, uniforms, vocab, dtype)
+        check(cu, target, None, tokens, temperature, uniforms, vocab, dtype)
 
 
 def test_rows_behind_the_last_request_are_left_alone():
@@ -98,6 +106,41 @@ def test_acceptance_at_its_border(vocab, half):
         assert int(accepted) == takes
         # refused: the columns that the draft has none of keep all of their weight, the others nothing; the number 0 takes the first
         assert out.tolist() == ([vocab - 3, 0] if takes else [0, -1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_borders_in_batches_whose_sums_are_made_in_32_bits_first(dtype):
+    """120 requests over 65536 columns: more than are summed in 64 bits at once.  Each request meets its border at several positions: even distributions, the draft's over half, a quarter, an
+    eighth of the columns, and numbers at the quotient, the next below and the next above."""
+    vocab, n = 65536, 3
+    steps = [0.5, 0.25, 0.125]
+    cu = ints(*range(0, 4 * 120 + 1, 4))
+    target = torch.full((480, vocab), 1.25, device=DEV, dtype=TDT[dtype])
+    draft = torch.full((360, vocab), -INF, device=DEV, dtype=TDT[dtype])
+    numbers, want, tokens = [], [], []
+    for b in range(120):
+        j = n
+        for i in range(n):
+            ratio = steps[(b + i) % 3]
+            draft[3 * b + i, :int(vocab * ratio)] = -2.5
+            kind = (b // 3 + 2 * i * (b % 5)) % 3
+            u = [float(torch.nextafter(torch.tensor(ratio), torch.tensor(0.0))), ratio, float(torch.nextafter(torch.tensor(ratio), torch.tensor(1.0)))][kind]
+            j = min(j, i) if kind else j
+            numbers.append(u), tokens.append((977 * b + i) % int(vocab * ratio))
+        k = (613 * b) % 1024           # the emitted token at a border too
+        numbers.append(k / 1024)
+        if j == n:
+            token = 64 * k
+        else:                          # p - q is left where the draft has nothing
+            ratio = steps[(b + j) % 3]
+            first, left = int(vocab * ratio), vocab - int(vocab * ratio)
+            token = first + math.floor(k / 1024 * left)
+            if (k * left) % 1024:      # (between two columns there is no border)
+                token = first + k * left // 1024
+        want += tokens[3 * b:3 * b + j] + [token] + [-1] * (n - j)
+    accepted, out = run_verify(cu, target, draft, ints(*tokens), None, floats(*numbers), vocab, dtype)
+    assert out.tolist() == want
+    assert 0 < int(accepted.sum()) < 360
 
 
 @pytest.mark.parametrize("vocab", [1024, 16384, 131072])
