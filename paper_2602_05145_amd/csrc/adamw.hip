@@ -11,9 +11,8 @@ namespace tide {
 namespace {
 
 constexpr int kWide = 4;                            // consecutive elements of a thread: a wave's accesses are one piece of memory each
-constexpr int kPerThread = 8;                       // in two lots
 constexpr int kThreads = 256;
-constexpr int kPerBlock = kPerThread * kThreads;    // 2048 elements of one tensor
+constexpr int kPerBlock = kWide * kThreads;         // 1024 elements of one tensor
 constexpr int kScaled = 256;                        // elements that share a scale: 32 lanes
 constexpr int kPerLaunch = 44;                      // tensors whose table fits the 4 KB of a launch's arguments
 constexpr double kLastCache = 288 << 20;            // bytes from which on nothing is left there for the next call
@@ -110,28 +109,54 @@ __device__ __forceinline__ void decode(uint32_t c, float scale, float (&x)[4]) {
   x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
 }
 
-// The codes of four of a block's numbers, of which a wave holds all.  x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
-// often as it lies beyond the lower: `coin` holds 16 random bits for each.  (To the nearest, a second moment would stand still: a step moves it by up to
-// 1 - beta2 of itself, and the codes lie 6 to 12 % apart.)  Numbers that are not finite become NaN and leave the others alone.
-__device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&coin)[4], bool upper, float& scale) {
-  float top = 0.f;
+// The codes of four of a block's numbers, of which a wave holds all: x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
+// often as it lies beyond the lower: `coin` holds 16 random bits for each, the lower half for the one, the upper for the other.  (To the nearest, a second moment would stand still: a
+// step moves it by up to 1 - beta2 of itself, and the codes lie 6 to 12 % apart.)  Numbers that are not finite become NaN and leave the others alone.
+// A number times 2^-120 has e4m3's code in the upper bits of its fp32 form, subnormal numbers too: 20 bits go.  (8-bit moments take twice the instructions of 32-bit ones and keep
+// the vector unit as busy as memory: this form, whole numbers for the largest and one division for both scales took 124 of them per element to 93, and the large draft from 2575 to 2383 us.)
+// The block's largest magnitude, compared as the whole numbers that magnitudes' bits are in the same order as, behind which infinities and NaN come; odd: there are such.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false)); }
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
+  v = dpp_max<0x111, 0xf>(v);
+  v = dpp_max<0x112, 0xf>(v);
+  v = dpp_max<0x114, 0xf>(v);
+  v = dpp_max<0x118, 0xf>(v);
+  v = dpp_max<0x142, 0xa>(v);
+  v = dpp_max<0x143, 0xc>(v);
+  return __builtin_amdgcn_readlane(v, 63);
+}
+constexpr uint32_t kInf = 0x7F800000u;
+__device__ __forceinline__ float largest(const float (&x)[4], bool& odd) {
+  uint32_t u[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(x[j]) < INFINITY ? fabsf(x[j]) : 0.f);
-  top = fast_max(top);
-  if (!(top >= 0x1p-100f)) top = 0.f;   // (1 / top has to be a number)
-  const float factor = top > 0.f ? (1.f / top) * kTop : 0.f;   // (what this rounds moves the largest by a few of the 2^20 that `coin` covers)
-  scale = top * (1.f / kTop);
-  uint32_t c = 0;
+  for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+  uint32_t top = wave_max_bits(max(max(u[0], u[1]), max(u[2], u[3])));
+  odd = top >= kInf;
+  if (odd) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = u[j] < kInf ? u[j] : 0;
+    top = wave_max_bits(max(max(u[0], u[1]), max(u[2], u[3])));
+  }
+  return top >= (127u - 100u) << 23 ? __uint_as_float(top) : 0.f;   // from 2^-100 on: 1 / top has to be a number
+}
+template <bool UPPER>
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&coin)[4], float factor, bool odd) {
+  uint32_t u[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float y = fminf(fabsf(x[j]) * factor, kTop);
-    // below the smallest normal number, 2^-6, the codes are 2^-9 apart as they are up to 2^-5: one more in front makes them alike.  20 bits go.
-    const bool low = y < 0x1p-6f;
-    const uint32_t bits = __float_as_uint(low ? y + 0x1p-6f : y) + ((upper ? coin[j] >> 16 : coin[j] & 0xFFFFu) << 4) + 8;
-    const bool fine = fabsf(x[j]) < INFINITY;
-    c |= (fine ? ((bits >> 20) - (low ? 968 : 960)) | (x[j] < 0.f ? 0x80u : 0u) : 0x7Fu) << (8 * j);
+    const float y = fminf(fabsf(x[j]) * factor, kTop) * 0x1p-120f;
+    const uint32_t extra = UPPER ? (coin[j] >> 12) & 0xFFFF0u : (coin[j] << 4) & 0xFFFF0u;
+    u[j] = (__float_as_uint(y) + extra + 8) << 4;                                   // the code in the upper byte
+    if constexpr (!UPPER) u[j] = (u[j] & 0x7FFFFFFFu) | (__float_as_uint(x[j]) & 0x80000000u);   // (what is in the upper half, roots, has no sign)
   }
-  return c;
+  if (__builtin_expect(odd, 0)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if ((__float_as_uint(x[j]) & 0x7FFFFFFFu) >= kInf) u[j] = 0x7F000000u;
+  }
+  const uint32_t lo = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0703u), hi = __builtin_amdgcn_perm(u[3], u[2], 0x0C0C0703u);
+  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 
 // One element; every operation rounds by itself, so that the bits do not hang on how a compiler joins them.
@@ -146,67 +171,63 @@ __device__ __forceinline__ void update(const Rate& r, float g, float& m, float& 
 
 struct Step { Rate r; const float* grad_scale; uint32_t key; };
 
-// 2048 elements of one tensor from element `base` on, in lots of 1024: a wave has one block of 256 of each.  WHOLE: all are there, and every load is under way before the first
-// is waited for.
+// 1024 elements of one tensor from element `base` on: a wave has one block of 256.  WHOLE: all are there, and every load is under way before the first is waited for.
+// (Two and four lots a thread: the small draft 641 -> 663 -> 665 us, the large one 2575 -> 2565 -> 2630.)
 template <typename P, typename G, bool EIGHT, bool ONCE, bool WHOLE>
 __device__ __forceinline__ void work(const Entry& t, const Step& s, int64_t base) {
 #pragma clang fp contract(off)
-  constexpr int N = kPerThread / kWide;
   constexpr bool BF16 = sizeof(P) == 2;
   using X = Four<WHOLE, ONCE>;
   float* weights = BF16 ? t.master : (float*)t.param;
-  float g[N][4], w[N][4], m[N][4], v[N][4], root[4], sm[N], sv[N];
-  uint32_t cm[N], cv[N];
-  int64_t i[N];
-  int count[N];
+  float g[4], w[4], m[4], v[4], root[4], sm, sv;
+  uint32_t cm, cv;
+  const int64_t i = base + threadIdx.x * kWide, block = (WHOLE ? i : min(i, t.n - 1)) / kScaled;
+  const int count = WHOLE ? kWide : (int)min(max(t.n - i, (int64_t)0), (int64_t)kWide);
+  X::load((const G*)t.grad + i, count, g);
+  X::load(weights + i, count, w);
+  if constexpr (EIGHT) {
+    cm = X::load((const uint8_t*)t.m + i, count);
+    cv = X::load((const uint8_t*)t.v + i, count);
+    sm = t.m_scale[block], sv = t.v_scale[block];
+  } else {
+    X::load((const float*)t.m + i, count, m);
+    X::load((const float*)t.v + i, count, v);
+  }
+  if constexpr (EIGHT) {
+    decode(cm, sm, m);
+    decode(cv, sv, v);
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    i[k] = base + k * (kThreads * kWide) + threadIdx.x * kWide;
-    count[k] = WHOLE ? kWide : (int)min(max(t.n - i[k], (int64_t)0), (int64_t)kWide);
-    X::load((const G*)t.grad + i[k], count[k], g[k]);
-    X::load(weights + i[k], count[k], w[k]);
-    if constexpr (EIGHT) {
-      cm[k] = X::load((const uint8_t*)t.m + i[k], count[k]);
-      cv[k] = X::load((const uint8_t*)t.v + i[k], count[k]);
-      const int64_t block = (WHOLE ? i[k] : min(i[k], t.n - 1)) / kScaled;
-      sm[k] = t.m_scale[block], sv[k] = t.v_scale[block];
-    } else {
-      X::load((const float*)t.m + i[k], count[k], m[k]);
-      X::load((const float*)t.v + i[k], count[k], v[k]);
-    }
+    for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
+  }
+  if (s.grad_scale) {
+    const float f = *s.grad_scale;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] *= f;
   }
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    if constexpr (EIGHT) {
-      decode(cm[k], sm[k], m[k]);
-      decode(cv[k], sv[k], v[k]);
+  for (int j = 0; j < 4; ++j) update(s.r, g[j], m[j], v[j], root[j], w[j]);
+  X::store(weights + i, count, w);
+  if constexpr (BF16) X::store((bf16_t*)t.param + i, count, w);
+  if constexpr (EIGHT) {
+    const uint32_t key = s.key + (uint32_t)i + (uint32_t)((uint64_t)i >> 32) * 0x9E3779B9u;
+    uint32_t coin[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[k][j] = v[k][j] * v[k][j];
+    for (int j = 0; j < 4; ++j) {
+      coin[j] = mix(key + j);   // (i is a multiple of four: its upper half is the same for all)
+      if (!WHOLE && j >= count) m[j] = root[j] = 0.f;
     }
-    if (s.grad_scale) {
-      const float f = *s.grad_scale;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) g[k][j] *= f;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) update(s.r, g[k][j], m[k][j], v[k][j], root[j], w[k][j]);
-    X::store(weights + i[k], count[k], w[k]);
-    if constexpr (BF16) X::store((bf16_t*)t.param + i[k], count[k], w[k]);
-    if constexpr (EIGHT) {
-      const uint32_t key = s.key + (uint32_t)i[k] + (uint32_t)((uint64_t)i[k] >> 32) * 0x9E3779B9u;
-      uint32_t coin[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        coin[j] = mix(key + j);   // (i is a multiple of four: its upper half is the same for all)
-        if (!WHOLE && j >= count[k]) m[k][j] = root[j] = 0.f;
-      }
-      X::store((uint8_t*)t.m + i[k], count[k], encode(m[k], coin, false, sm[k]));
-      X::store((uint8_t*)t.v + i[k], count[k], encode(root, coin, true, sv[k]));
-      if (count[k] > 0 && threadIdx.x % (kScaled / kWide) == 0) t.m_scale[i[k] / kScaled] = sm[k], t.v_scale[i[k] / kScaled] = sv[k];
-    } else {
-      X::store((float*)t.m + i[k], count[k], m[k]);
-      X::store((float*)t.v + i[k], count[k], v[k]);
-    }
+    bool odd_m, odd_v;
+    const float top_m = largest(m, odd_m), top_v = largest(root, odd_v);
+    // one division for both: the lower half of the wave makes m's factor
+    const float top = (threadIdx.x & 32) ? top_v : top_m;
+    const float factor = top > 0.f ? (1.f / top) * kTop : 0.f;   // (what this rounds moves the largest by a few of the 2^20 that `coin` covers)
+    const float factor_m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), 0)), factor_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), 63));
+    X::store((uint8_t*)t.m + i, count, encode<false>(m, coin, factor_m, odd_m));
+    X::store((uint8_t*)t.v + i, count, encode<true>(root, coin, factor_v, odd_v));
+    if (count > 0 && threadIdx.x % (kScaled / kWide) == 0) t.m_scale[block] = top_m * (1.f / kTop), t.v_scale[block] = top_v * (1.f / kTop);
+  } else {
+    X::store((float*)t.m + i, count, m);
+    X::store((float*)t.v + i, count, v);
   }
 }
 template <typename P, typename G, bool EIGHT, bool ONCE>
@@ -215,7 +236,7 @@ __device__ __forceinline__ void work(const Entry& t, const Step& s, int64_t base
   else work<P, G, EIGHT, false, false>(t, s, base);
 }
 
-// Block b works on 2048 elements of the tensor its index falls in.  Bound by memory.  Past the caches (both ways) where a launch moves more than they hold: the small draft of
+// Block b works on 1024 elements of the tensor its index falls in.  Bound by memory.  Past the caches (both ways) where a launch moves more than they hold: the small draft of
 // 216M weights, 32 bits, 702 -> 674 us (5.6 TB/s), the large one of 794M, 8 bits, 2750 -> 2555; 2M weights, which the last cache holds, 10.2 -> 11.2.
 template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const Table a) {
