@@ -491,25 +491,26 @@ struct Source {
     if (zq) x.q.load(zq, col, V);
   }
   __device__ __forceinline__ void weigh(int64_t col, Columns& x, double (&w)[8]) const {   // by a whole wave
+#pragma clang fp contract(off)   // (equal probabilities leave nothing)
     float z[8], y[8];
     x.p.get(col, V, z);
     if (all_near(ep, z)) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = ep.near(z[k]) * ip;
+      for (int k = 0; k < 8; ++k) w[k] = ep.near(z[k]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = ep.of(z[k]) * ip;
+      for (int k = 0; k < 8; ++k) w[k] = ep.of(z[k]);
     }
     if (zq) {
       x.q.get(col, V, y);
       if (all_near(eq, y)) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.near(y[k]), iq, w[k]), 0.0);
+        for (int k = 0; k < 8; ++k) w[k] = fmax(w[k] * ip - eq.near(y[k]) * iq, 0.0);
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.of(y[k]), iq, w[k]), 0.0);
+        for (int k = 0; k < 8; ++k) w[k] = fmax(w[k] * ip - eq.of(y[k]) * iq, 0.0);
       }
-    } else {
+    } else if (__ballot(taken >= col && taken < col + 8)) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) w[k] = col + k == taken ? 0.0 : w[k];
     }
@@ -627,7 +628,7 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a, int
   if (at >= 0) {
     begin = at * unit, finish = min(begin + unit, a.V);
   } else {   // nothing weighs anything (a number of 1 and more refused what both distributions agree on): from the target's alone
-    border = number * d.sum * s.ip, before = 0.0, begin = 0;
+    border = number * d.sum, before = 0.0, begin = 0;
     s.zq = nullptr, s.taken = -1;
   }
   int64_t token = -1;

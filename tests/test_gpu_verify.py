@@ -175,6 +175,12 @@ def test_numbers_outside_of_their_range():
     assert accepted.tolist() == [0] and out.tolist() == [150, -1]
     accepted, out = run_verify(ints(0, 2), target[:2], target[:1].clone(), ints(150), None, floats(NAN, 0.995), vocab, "fp32")
     assert accepted.tolist() == [0] and out.tolist() == [199, -1]
+    # also where probabilities are no round numbers, and in a batch
+    for lens in ([1] * 3, [1] * 200):
+        cu, target, _, tokens, temperature, uniforms = batch(lens, 32001, "bf16", 41)
+        draft = target[cu[:-1].long()].contiguous()
+        uniforms[::2] = 1.0
+        check(cu, target, draft, tokens, temperature, uniforms, 32001, "bf16")
 
 
 def test_tokens_that_are_none_end_the_draft():
