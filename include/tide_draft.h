@@ -505,7 +505,7 @@ typedef struct tide_adamw_tensor {
   const void *grad;    /* of grad_dtype */
   void *m, *v;         /* moments: float for state_bits 32; for 8 one byte each, see below */
   float *m_scale, *v_scale;   /* state_bits 8: ceil(n / 256) scales each; else ignored */
-  int64_t n;           /* 0 ... 2^34; 0: the pointers may be NULL */
+  int64_t n;           /* 0 ... 2^33; 0: the pointers may be NULL */
   float weight_decay;  /* decoupled; 0 for tensors that are not decayed */
   int32_t param_dtype, grad_dtype, state_bits;
 } tide_adamw_tensor;
@@ -524,7 +524,8 @@ typedef struct tide_adamw_tensor {
  *
  * tide_adamw_dev takes the schedule from DEVICE memory, can be captured and replayed: it reads *lr_dev, uses and advances *step_dev, and writes `schedule` (DEVICE
  * scratch of 4 floats, 16-byte aligned; calls that overlap need one each).  Both forms give the same bits.
- * beta1 and beta2 in [0, 1), eps and weight_decay finite and >= 0, lr finite.  Enqueues kernels on `stream` and nothing else: one for each 44 tensors. */
+ * beta1 and beta2 in [0, 1), eps and weight_decay finite and >= 0, lr finite.  Enqueues kernels on `stream` and nothing else: one for each 44 tensors (and, the
+ * schedule on the device, one in front). */
 int tide_adamw(int32_t n_tensors, const tide_adamw_tensor *tensors, float lr, float beta1, float beta2, float eps,
                int64_t step, const float *grad_scale, uint32_t seed, void *stream);
 int tide_adamw_dev(int32_t n_tensors, const tide_adamw_tensor *tensors, const float *lr_dev, int64_t *step_dev, float beta1,

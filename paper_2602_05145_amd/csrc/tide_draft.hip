@@ -1334,7 +1334,7 @@ static int adamw(int32_t n_tensors, const tide_adamw_tensor* tensors, AdamwListA
   if (((uintptr_t)a.grad_scale) & 3) return fail(TIDE_ERR_CONFIG, "grad_scale must be 4-byte aligned");
   for (int32_t i = 0; i < n_tensors; ++i) {
     const tide_adamw_tensor& t = tensors[i];
-    if (t.n < 0 || t.n > ((int64_t)1 << 34)) return fail(TIDE_ERR_CONFIG, "tensor %d: n must be in [0, 2^34]", i);
+    if (t.n < 0 || t.n > ((int64_t)1 << 33)) return fail(TIDE_ERR_CONFIG, "tensor %d: n must be in [0, 2^33]", i);   // (a launch holds fewer than 2^32 threads, four elements each)
     if ((t.param_dtype != TIDE_DTYPE_FP32 && t.param_dtype != TIDE_DTYPE_BF16) || (t.grad_dtype != TIDE_DTYPE_FP32 && t.grad_dtype != TIDE_DTYPE_BF16))
       return fail(TIDE_ERR_CONFIG, "tensor %d: bad dtype", i);
     if (t.state_bits != 32 && t.state_bits != 8) return fail(TIDE_ERR_CONFIG, "tensor %d: state_bits must be 32 or 8", i);
@@ -1354,7 +1354,7 @@ static int adamw(int32_t n_tensors, const tide_adamw_tensor* tensors, AdamwListA
 
 int tide_adamw(int32_t n_tensors, const tide_adamw_tensor* tensors, float lr, float beta1, float beta2, float eps, int64_t step, const float* grad_scale, uint32_t seed,
                void* stream) {
-  if (step < 0 || !std::isfinite(lr)) return fail(TIDE_ERR_CONFIG, "step must not be negative, and lr must be finite");
+  if (step < 0 || step == INT64_MAX || !std::isfinite(lr)) return fail(TIDE_ERR_CONFIG, "step must be in [0, 2^63 - 1), and lr finite");
   AdamwListArgs a{};
   a.beta1 = beta1, a.beta2 = beta2, a.eps = eps, a.lr = lr, a.step = step, a.grad_scale = grad_scale, a.seed = seed;
   return adamw(n_tensors, tensors, a, stream);

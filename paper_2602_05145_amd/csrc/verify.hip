@@ -127,22 +127,29 @@ __device__ __forceinline__ bool all_near(const Scale& e, const float (&z)[8]) {
 
 // The request that a row belongs to, the first that ends behind it, by a wave; a.requests where there is none.
 __device__ __forceinline__ int owner_of(const VerifyArgs& a, int64_t row, bool of_target, int lane) {
-  for (int b0 = 0; b0 < a.requests; b0 += 256) {
-    int end[4];
+  auto behind = [&](int end, int k) { return (int64_t)end - (of_target ? 0 : k + 1) > row; };
+  int lo = 0, hi = a.requests;   // it is among these, or behind them
+  while (hi - lo > 256) {
+    const int step = (hi - lo + 63) / 64, k = min(lo + (lane + 1) * step, hi) - 1;
+    const unsigned long long ends = __ballot(behind(a.cu[k + 1], k));
+    if (!ends) return a.requests;
+    lo += (__ffsll(ends) - 1) * step;
+    hi = min(lo + step, hi);
+  }
+  int end[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) end[u] = a.cu[min(b0 + 64 * u + lane, a.requests - 1) + 1];
+  for (int u = 0; u < 4; ++u) end[u] = a.cu[min(lo + 64 * u + lane, hi - 1) + 1];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = b0 + 64 * u + lane;
-      const unsigned long long ends = __ballot(k < a.requests && (int64_t)end[u] - (of_target ? 0 : k + 1) > row);
-      if (ends) return b0 + 64 * u + __ffsll(ends) - 1;
-    }
+  for (int u = 0; u < 4; ++u) {
+    const int k = lo + 64 * u + lane;
+    const unsigned long long ends = __ballot(k < hi && behind(end[u], k));
+    if (ends) return lo + 64 * u + __ffsll(ends) - 1;
   }
   return a.requests;
 }
 
 // Temperatures for which sums in 32 bits are good to kNear / 4.  An exponent c (z - top) takes three roundings, |t| 2^-23.4 of its power; with up to 2^28 columns those that
-// make a difference have |t| <= 28 and so 2^-18.6.  A thread adds 64 of them, 2^-18.  At the ends of fp32 c itself loses bits.
+// make a difference have |t| <= 28 and so 2^-18.6.  A thread adds 16 sums of eight, each moved to a new maximum at most as often: 2^-19.  At the ends of fp32 c itself loses bits.
 __device__ __forceinline__ bool rough_ok(float tau) { return tau >= 0x1p-100f && tau <= 0x1p100f; }
 
 // Of U * 2048 columns of one row: the largest value and the sum of exponentials beside it, in 64 bits.

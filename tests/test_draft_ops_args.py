@@ -73,7 +73,7 @@ def test_embedding_workspace_never_falls_as_rows_grow(d):
 
 
 @pytest.mark.parametrize("dev", [False, True])
-@pytest.mark.parametrize("bad", [dict(n=-1), dict(n=(1 << 34) + 1), dict(param_dtype=2), dict(grad_dtype=-1), dict(state_bits=16), dict(weight_decay=-0.1), dict(weight_decay=NAN),
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(n=(1 << 33) + 1), dict(param_dtype=2), dict(grad_dtype=-1), dict(state_bits=16), dict(weight_decay=-0.1), dict(weight_decay=NAN),
                                  dict(weight_decay=INF), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0), dict(beta2=NAN), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF),
                                  dict(grad_scale=P + 2), dict(master=P + 2), dict(param=P + 1), dict(grad=P + 2), dict(grad_dtype=BF16, grad=P + 1), dict(m_scale=P + 1),
                                  dict(state_bits=32, m=P + 2), dict(param_dtype=F32, param=P + 2)], ids=str)
@@ -84,7 +84,7 @@ def test_adamw_refuses(bad, dev):
 def test_adamw_refuses_pointers_and_schedules():
     for name in ("param", "master", "grad", "m", "v", "m_scale", "v_scale"):
         assert adamw(**{name: None}) == B.TIDE_ERR_NULL, name
-    assert adamw(step=-1) == adamw(lr=NAN) == adamw(lr=INF) == B.TIDE_ERR_CONFIG
+    assert adamw(step=-1) == adamw(step=2 ** 63 - 1) == adamw(lr=NAN) == adamw(lr=INF) == B.TIDE_ERR_CONFIG
     assert B.lib().tide_adamw(1, None, 0.1, 0.9, 0.99, 1e-8, 0, None, 1, None) == B.TIDE_ERR_NULL
     assert B.lib().tide_adamw(-1, entry(), 0.1, 0.9, 0.99, 1e-8, 0, None, 1, None) == B.TIDE_ERR_CONFIG
     for missing in range(3):

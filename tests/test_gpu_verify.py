@@ -72,6 +72,13 @@ def test_numbers_of_requests_and_drafts(lens):
         assert max(got) > 0 and any(a < n for a, n in zip(got, lens))
 
 
+@pytest.mark.parametrize("requests", [257, 5000, 20000])
+def test_many_requests(requests):
+    """More than are looked through at once for the one that a row belongs to."""
+    lens = [(b * b + b // 7) % 4 for b in range(requests)]
+    check(*batch(lens, 40, "fp32", requests, near=0.5), 40, "fp32")
+
+
 def test_large_batches_take_wider_parts():
     """Rows enough for wider parts, for sums in 32 bits first, and for parts of 16384 and 32768 columns; requests without sampling, without a distribution and at
     temperatures for which 32 bits are no good among them; a draft and none."""
