@@ -11,6 +11,9 @@ namespace {
 constexpr int kCols = 512;        // columns of a wave: eight a lane
 constexpr int kChunk = 2048;      // rows that a block sorts
 constexpr int kWays = 16;         // sorted runs that a pass joins
+constexpr int kJoin = 16;         // pieces that a block joins
+constexpr int kAlone = 16;        // parts of a token that one wave adds up
+static_assert(kAlone >= kJoin);
 constexpr int kIdBits = 21;       // ids are below 2^21, and a chunk's place takes the 11 bits behind them
 constexpr uint32_t kNone = (1u << kIdBits) - 1;   // id of a row without a token; no vocabulary reaches it
 static_assert(kIdBits + 11 == 32 && kChunk == 1 << 11);
@@ -39,27 +42,36 @@ template <typename T> __device__ __forceinline__ void add8(const Loose8<T>& raw,
   for (int j = 0; j < 8; ++j) sum[j] += x[j];
 }
 
-// One wave copies G * kCols columns of a row, all of its loads under way together.
-template <typename T, int G, bool TINY>
+// One wave copies G * kCols columns of R rows that follow each other, all of its loads under way together: 32665 rows of 232 columns with a wave for each four in 7.6 us, for each
+// one 9.1.
+template <typename T, int G, int R, bool TINY>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(int64_t rows, int vocab, int d, int tiles, const int32_t* __restrict__ ids, const T* __restrict__ table,
                                                         float scale, T* __restrict__ out) {
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t row = w / tiles;
+  const int64_t row = w / tiles * R;
   if (row >= rows) return;
   const int c = (int)(w % tiles) * (G * kCols) + (threadIdx.x & 63) * 8;
-  const int id = __builtin_amdgcn_readfirstlane(ids[row]);
-  const bool some = id >= 0 && id < vocab;
-  const T* from = table + (size_t)(some ? id : 0) * d;
-  Loose8<T> raw[G];
+  bool some[R];
+  Loose8<T> raw[R][G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) Lane<TINY>(c + g * kCols, d).load(raw[g], from);
+  for (int r = 0; r < R; ++r) {
+    const int id = __builtin_amdgcn_readfirstlane(ids[min(row + r, rows - 1)]);
+    some[r] = id >= 0 && id < vocab;
+    const T* from = table + (size_t)(some[r] ? id : 0) * d;
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    float x[8];
-    raw[g].get(x);
+    for (int g = 0; g < G; ++g) Lane<TINY>(c + g * kCols, d).load(raw[r][g], from);
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = some ? x[j] * scale : 0.f;
-    Lane<TINY>(c + g * kCols, d).store(out + (size_t)row * d, x);
+  for (int r = 0; r < R; ++r) {
+    if (row + r >= rows) return;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float x[8];
+      raw[r][g].get(x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = some[r] ? x[j] * scale : 0.f;
+      Lane<TINY>(c + g * kCols, d).store(out + (size_t)(row + r) * d, x);
+    }
   }
 }
 
@@ -101,7 +113,8 @@ __device__ __forceinline__ void sort_chunk(uint32_t (&key)[8], uint32_t* lds) {
 }
 
 // The first `chunks` blocks sort kChunk ids each, with their places, by id and then by place (no two keys are alike: there is one order); the others clear the gradient, where it
-// is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.
+// is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.  Past the caches: the write-back of
+// plain stores falls into the launches that follow (38.4 MB with 3968 rows of 192: 37 us in all, 34 past them).
 __global__ __launch_bounds__(256) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
                                                          int32_t* __restrict__ pos, uint8_t* __restrict__ clear, size_t head, size_t words, int tail) {
   if (blockIdx.x >= chunks) {
@@ -232,52 +245,97 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece
   }
 }
 
-// Adds up the parts of a token that reaches over pieces, from the piece it begins in.
-template <typename G, bool ADD, bool TINY>
-__global__ __launch_bounds__(256) void embed_join_kernel(int64_t total, int piece, int d, int tiles, const uint32_t* __restrict__ sid, float scale, G* __restrict__ dtable,
-                                                         const float* __restrict__ parts) {
+// Adds up `n` parts of a token, those of the pieces behind `p`, in front of which `sum` holds what came before.
+template <bool TINY>
+__device__ __forceinline__ void add_parts(const Lane<TINY>& own, const float* __restrict__ parts, int64_t p, int n, int d, float (&sum)[8]) {
   constexpr int U = 8;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t p = w / tiles, end = (p + 1) * piece;
-  if (end >= total) return;   // nothing goes on behind the last one
-  const int lane = threadIdx.x & 63;
-  const uint32_t before = p > 0 ? sid[p * piece - 1] : kNone, id = sid[end - 1];
-  const int64_t reach = end + (int64_t)lane * piece;
-  const uint32_t starts = reach < total ? sid[reach] : kNone;   // what the pieces behind begin with
-  if (id == kNone || id == before) return;                      // begins before
-  unsigned long long goes_on = __ballot(starts == id);
-  if (!(goes_on & 1)) return;
-  const Lane<TINY> own((int)(w % tiles) * kCols + lane * 8, d);
-  float sum[8], x[8];
-  Loose8<G> old;
-  Loose8<float> begun;
-  if constexpr (ADD) own.load(old, dtable + (size_t)id * d);
-  own.load(begun, parts + (size_t)(2 * p + 1) * d);
-  begun.get(sum);
-  for (int64_t q = p + 1;;) {
-    const int n = ~goes_on ? __ffsll(~goes_on) - 1 : 64;   // pieces from q on that the token reaches into
-    for (int k = 0; k < n; k += U) {
-      Loose8<float> raw[U];
+  for (int k = 0; k < n; k += U) {
+    Loose8<float> raw[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) own.load(raw[u], parts + (size_t)(2 * (q + min(k + u, n - 1))) * d);
+    for (int u = 0; u < U; ++u) own.load(raw[u], parts + (size_t)(2 * (p + 1 + min(k + u, n - 1))) * d);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k + u < n) add8(raw[u], sum);
+    for (int u = 0; u < U; ++u)
+      if (k + u < n) add8(raw[u], sum);
+  }
+}
+
+// Adds up the parts of a token that reaches over pieces, from the piece it begins in: kJoin pieces a block, one a wave, for the same 512 columns.  A wave adds up to kAlone parts
+// by itself; those of a token with more are divided between the block's waves, whose sums are added in their order.  (Behind a token of that many parts the next one begins in
+// another block.)  32665 rows of 232 columns of which one token has 2700: 10 us, 36 where one wave adds them all up.
+template <typename G, bool ADD, bool TINY>
+__global__ __launch_bounds__(64 * kJoin) void embed_join_kernel(int64_t total, int piece, int d, const uint32_t* __restrict__ sid, float scale,
+                                                                G* __restrict__ dtable, const float* __restrict__ parts) {
+  __shared__ float lds[kJoin][kCols];
+  __shared__ int who, many;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t begin = (int64_t)blockIdx.x * kJoin, p = begin + wave, end = (p + 1) * piece;
+  const Lane<TINY> own((int)blockIdx.y * kCols + lane * 8, d);
+  if (threadIdx.x == 0) many = 0;
+  __syncthreads();
+  uint32_t id = kNone;
+  int n = 0;   // pieces behind p that its last token reaches into, where it begins in p
+  if (end < total) {
+    id = sid[end - 1];
+    const uint32_t before = p > 0 ? sid[p * piece - 1] : kNone;
+    const int64_t reach = end + (int64_t)lane * piece;
+    const unsigned long long goes_on = __ballot((reach < total ? sid[reach] : kNone) == id);   // (of what the pieces behind begin with)
+    if (id != kNone && id != before) n = ~goes_on ? __ffsll(~goes_on) - 1 : 64;
+    if (n == 64) {   // the ids ascend: the number is found by a search of 64 ways
+      int64_t more = total / piece - (p + 1) - 64, from = 64;   // (total is a multiple of every piece)
+      while (more > 0) {
+        const int64_t step = (more + 63) / 64, at = (lane + 1) * step;
+        const int whole = __popcll(__ballot(at <= more && sid[at <= more ? (p + from + at) * piece : 0] == id));
+        from += whole * step;
+        more = min(more - whole * step, step - 1);
+      }
+      n = (int)from;
     }
-    if (n < 64) break;
-    q += 64;
-    const int64_t next = (q + lane) * piece;
-    goes_on = __ballot((next < total ? sid[next] : kNone) == id);
   }
-  if constexpr (ADD) {
-    old.get(x);
+  auto store = [&](uint32_t id, const Loose8<G>& old, float (&sum)[8]) {
+    float x[8];
+    if constexpr (ADD) {
+      old.get(x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
-  } else {
+      for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
+      for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
+    }
+    own.store(dtable + (size_t)id * d, x);
+  };
+  if (lane == 0 && n > kAlone) who = wave, many = n;
+  if (n > 0 && n <= kAlone) {
+    float sum[8];
+    Loose8<G> old;
+    Loose8<float> begun;
+    if constexpr (ADD) own.load(old, dtable + (size_t)id * d);
+    own.load(begun, parts + (size_t)(2 * p + 1) * d);
+    begun.get(sum);
+    add_parts(own, parts, p, n, d, sum);
+    store(id, old, sum);
   }
-  own.store(dtable + (size_t)id * d, x);
+  __syncthreads();
+  if (many == 0) return;
+  const int each = (many + kJoin - 1) / kJoin, from = min(wave * each, many);
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  Loose8<G> old;
+  if (wave == who) {
+    Loose8<float> begun;
+    if constexpr (ADD) own.load(old, dtable + (size_t)id * d);
+    own.load(begun, parts + (size_t)(2 * p + 1) * d);
+    begun.get(sum);
+  }
+  add_parts(own, parts, begin + who + from, min(each, many - from), d, sum);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) lds[wave][j * 64 + lane] = sum[j];
+  __syncthreads();
+  if (wave != who) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+  for (int k = 0; k < kJoin; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += lds[k][j * 64 + lane];
+  store(id, old, sum);
 }
 
 struct Plan {
@@ -313,7 +371,8 @@ hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const
   }
   if (p.pieces < 2) return hipSuccess;
   ProfScope ps("embed_join", 0, 0, s);
-  hipLaunchKernelGGL((embed_join_kernel<G, ADD, TINY>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, a.scale, (G*)a.dtable, parts);
+  hipLaunchKernelGGL((embed_join_kernel<G, ADD, TINY>), dim3((unsigned)((p.pieces + kJoin - 1) / kJoin), p.tiles), dim3(64 * kJoin), 0, s, p.total, p.piece, (int)a.d, sid,
+                     a.scale, (G*)a.dtable, parts);
   return hipGetLastError();
 }
 
@@ -325,13 +384,16 @@ hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const
 
 template <typename T>
 hipError_t embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, const T* table, float scale, T* out, hipStream_t s) {
-  // few rows: a wave for each 512 columns; many: for each 2048
-  const bool few = rows * ((d + kCols - 1) / kCols) < 16384;
-  const int wide = few ? kCols : 4 * kCols, tiles = (d + wide - 1) / wide;
-  const unsigned blocks = (unsigned)((rows * tiles + 3) / 4);
-  if (d < 8) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, true>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, rows, vocab, d, 1, ids, table, scale, out);
-  else if (few) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, false>), dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, table, scale, out);
-  else hipLaunchKernelGGL((embed_fwd_kernel<T, 4, false>), dim3(blocks), dim3(256), 0, s, rows, vocab, d, tiles, ids, table, scale, out);
+  // few rows: a wave for each 512 columns; many: for each 2048, of four rows where a row has no more than 512
+  const int least = (d + kCols - 1) / kCols;
+  const bool few = rows * least < 16384, narrow = least == 1;
+  const int tiles = few ? least : (d + 4 * kCols - 1) / (4 * kCols);
+  const int64_t waves = few || !narrow || d < 8 ? rows * tiles : (rows + 3) / 4;
+  const dim3 grid((unsigned)((waves + 3) / 4)), block(256);
+  if (d < 8) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 1, true>), grid, block, 0, s, rows, vocab, d, 1, ids, table, scale, out);
+  else if (few) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 1, false>), grid, block, 0, s, rows, vocab, d, tiles, ids, table, scale, out);
+  else if (narrow) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 4, false>), grid, block, 0, s, rows, vocab, d, 1, ids, table, scale, out);
+  else hipLaunchKernelGGL((embed_fwd_kernel<T, 4, 1, false>), grid, block, 0, s, rows, vocab, d, tiles, ids, table, scale, out);
   return hipGetLastError();
 }
 

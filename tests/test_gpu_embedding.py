@@ -110,6 +110,24 @@ def test_gradient_of_many_rows(rows):
     check_gradient(make_ids(rows, 5000, "frequent", 4), "bf16", "fp32", 5000, 24, False, repeat=True)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dtype,out,d", [("fp32", "fp32", 24), ("bf16", "bf16", 515), ("bf16", "fp32", 3)])
+def test_gradient_of_tokens_over_many_pieces(dtype, out, d, accumulate):
+    """Tokens whose rows reach over as many pieces of eight rows as one wave adds up, one more, as one probe sees, one more, and far more, ending at a piece's end and in it."""
+    lengths = [8 * pieces + rest for pieces in (1, 15, 16, 17, 18, 32, 63, 64, 65, 66, 128, 129, 130, 257) for rest in (0, 1, 7)]
+    ids = torch.repeat_interleave(torch.arange(len(lengths), device=DEV), torch.tensor(lengths, device=DEV)).to(torch.int32)
+    ids = ids[torch.randperm(ids.numel(), device=DEV, generator=gen(3))]
+    check_gradient(ids, dtype, out, len(lengths) + 2, d, accumulate, repeat=True)
+
+
+@pytest.mark.parametrize("rows,others", [(40000, 0), (300000, 0), (300000, 777), (32768, 1)])
+def test_gradient_of_one_token_in_most_rows(rows, others):
+    ids = torch.full((rows,), 40, dtype=torch.int32, device=DEV)
+    if others:
+        ids[torch.randperm(rows, device=DEV, generator=gen(4))[:others]] = torch.randint(0, 99, (others,), device=DEV, generator=gen(6), dtype=torch.int32)
+    check_gradient(ids, "bf16", "fp32", 99, 8, True, repeat=True)
+
+
 @pytest.mark.parametrize("off", [1, 2, 3, 5])
 @pytest.mark.parametrize("dtype,out", [("fp32", "fp32"), ("bf16", "bf16")])
 def test_gradient_of_arrays_that_begin_anywhere(off, dtype, out):
