@@ -109,11 +109,6 @@ __device__ __forceinline__ void decode(uint32_t c, float scale, float (&x)[4]) {
   x[0] = lo[0] * scale, x[1] = lo[1] * scale, x[2] = hi[0] * scale, x[3] = hi[1] * scale;
 }
 
-// The codes of four of a block's numbers, of which a wave holds all: x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
-// often as it lies beyond the lower: `coin` holds 16 random bits for each, the lower half for the one, the upper for the other.  (To the nearest, a second moment would stand still: a
-// step moves it by up to 1 - beta2 of itself, and the codes lie 6 to 12 % apart.)  Numbers that are not finite become NaN and leave the others alone.
-// A number times 2^-120 has e4m3's code in the upper bits of its fp32 form, subnormal numbers too: 20 bits go.  (8-bit moments take twice the instructions of 32-bit ones and keep
-// the vector unit as busy as memory: this form, whole numbers for the largest and one division for both scales took 124 of them per element to 93, and the large draft from 2575 to 2383 us.)
 // The block's largest magnitude, compared as the whole numbers that magnitudes' bits are in the same order as, behind which infinities and NaN come; odd: there are such.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ uint32_t dpp_max(uint32_t v) { return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false)); }
@@ -140,6 +135,11 @@ __device__ __forceinline__ float largest(const float (&x)[4], bool& odd) {
   }
   return top >= (127u - 100u) << 23 ? __uint_as_float(top) : 0.f;   // from 2^-100 on: 1 / top has to be a number
 }
+// The codes of four of a block's numbers, of which a wave holds all: x beside the block's largest magnitude (448 stands for it) is rounded to one of the two codes around it, up as
+// often as it lies beyond the lower: `coin` holds 16 random bits for each, the lower half for the one, the upper for the other.  (To the nearest, a second moment would stand still: a
+// step moves it by up to 1 - beta2 of itself, and the codes lie 6 to 12 % apart.)  Numbers that are not finite become NaN and leave the others alone.
+// A number times 2^-120 has e4m3's code in the upper bits of its fp32 form, subnormal numbers too: 20 bits go.  (8-bit moments take twice the instructions of 32-bit ones and keep
+// the vector unit as busy as memory: this form, whole numbers for the largest and one division for both scales took 124 of them per element to 93, and the large draft from 2575 to 2383 us.)
 template <bool UPPER>
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], const uint32_t (&coin)[4], float factor, bool odd) {
   uint32_t u[4];

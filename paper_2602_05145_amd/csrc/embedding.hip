@@ -9,12 +9,14 @@ namespace tide {
 namespace {
 
 constexpr int kCols = 512;        // columns of a wave: eight a lane
-constexpr int kChunk = 2048;      // rows that a block sorts
+constexpr int kChunk = 2048;      // rows that a block sorts, eight a thread; up to kWhole where one block then sorts all
+constexpr int kWhole = 4096;
 constexpr int kWays = 16;         // sorted runs that a pass joins
+constexpr int kFewRows = 128;     // rows of a backward pass without a sort
 constexpr int kJoin = 16;         // pieces that a block joins
 constexpr int kAlone = 16;        // parts of a token that one wave adds up
 static_assert(kAlone >= kJoin);
-constexpr int kIdBits = 21;       // ids are below 2^21, and a chunk's place takes the 11 bits behind them
+constexpr int kIdBits = 21;       // ids are below 2^21, and the place in a chunk takes the 11 bits behind them (12 of kWhole, for ids below 2^20)
 constexpr uint32_t kNone = (1u << kIdBits) - 1;   // id of a row without a token; no vocabulary reaches it
 static_assert(kIdBits + 11 == 32 && kChunk == 1 << 11);
 
@@ -40,6 +42,21 @@ template <typename T> __device__ __forceinline__ void add8(const Loose8<T>& raw,
   raw.get(x);
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum[j] += x[j];
+}
+
+// What a token's sum becomes: its row, or what is added to it.
+template <typename G, bool ADD, bool TINY>
+__device__ __forceinline__ void finish(const Lane<TINY>& own, const float (&sum)[8], const Loose8<G>& old, float scale, G* row) {
+  float x[8];
+  if constexpr (ADD) {
+    old.get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
+  }
+  own.store(row, x);
 }
 
 // One wave copies G * kCols columns of R rows that follow each other, all of its loads under way together: 32665 rows of 232 columns with a wave for each four in 7.6 us, for each
@@ -75,70 +92,96 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(int64_t rows, int vocab,
   }
 }
 
-// Bitonic order of kChunk keys, eight consecutive ones a thread: distances below 8 in a thread's registers, up to 256 between the lanes of a wave, 512 and 1024 through LDS.
+// Of two keys the smaller (side 0) or the larger (side 2^32 - 1): the middle one of three, one instruction.
+__device__ __forceinline__ uint32_t one_of(uint32_t a, uint32_t b, uint32_t side) { return max(min(a, b), min(max(a, b), side)); }
+// The key and that of the lane at distance LANES (a power of two), in either order.
+template <int LANES>
+__device__ __forceinline__ void pair(uint32_t key, uint32_t& a, uint32_t& b) {
+  a = key;
+  if constexpr (LANES == 1) b = __builtin_amdgcn_mov_dpp((int)key, 0xB1, 0xf, 0xf, true);         // within four lanes: 1 0 3 2, 2 3 0 1
+  else if constexpr (LANES == 2) b = __builtin_amdgcn_mov_dpp((int)key, 0x4E, 0xf, 0xf, true);
+  else if constexpr (LANES == 4) b = __builtin_amdgcn_ds_swizzle((int)key, 0x101F);
+  else if constexpr (LANES == 8) b = __builtin_amdgcn_mov_dpp((int)key, 0x128, 0xf, 0xf, true);   // a row of 16 turned by 8
+  else {
+    const auto r = LANES == 16 ? __builtin_amdgcn_permlane16_swap(key, key, false, false) : __builtin_amdgcn_permlane32_swap(key, key, false, false);
+    a = r[0], b = r[1];
+  }
+}
+// Bitonic order of CHUNK keys, eight consecutive ones a thread: distances below 8 in a thread's registers, up to 256 between the lanes of a wave, from 512 on through LDS.  Bound by
+// one CU's vector unit: an instruction for a choice and exchanges beside LDS take 3 us off 2048 keys.
+template <int CHUNK>
 __device__ __forceinline__ void sort_chunk(uint32_t (&key)[8], uint32_t* lds) {
   const int t = threadIdx.x;
-  auto keep = [&](int i, uint32_t other, int j, int k) {   // of a pair at distance j, the lower place keeps the smaller where its run of k ascends
-    const int e = t * 8 + i;
-    const bool smaller = ((e & j) == 0) == ((e & k) == 0);
-    key[i] = smaller ? min(key[i], other) : max(key[i], other);
-  };
 #pragma unroll
-  for (int k = 2; k <= kChunk; k *= 2) {
+  for (int k = 2; k <= CHUNK; k *= 2) {
 #pragma unroll
-    for (int j = kChunk / 2; j > 0; j /= 2) {
+    for (int j = CHUNK / 2; j > 0; j /= 2) {
       if (j >= k) continue;
+      // of a pair at distance j, the lower place keeps the smaller where its run of k ascends
+      const uint32_t turn = (t * 8) & k ? ~0u : 0u, side = (t * 8) & j ? ~turn : turn;
       if (j >= 512) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lds[i * 256 + t] = key[i];
+        for (int i = 0; i < 8; ++i) lds[i * (CHUNK / 8) + t] = key[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) keep(i, lds[i * 256 + (t ^ (j / 8))], j, k);
+        for (int i = 0; i < 8; ++i) key[i] = one_of(key[i], lds[i * (CHUNK / 8) + (t ^ (j / 8))], side);
       } else if (j >= 8) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) keep(i, __shfl_xor(key[i], j / 8, 64), j, k);
+        for (int i = 0; i < 8; ++i) {
+          uint32_t a, b;
+          if (j == 8) pair<1>(key[i], a, b);
+          else if (j == 16) pair<2>(key[i], a, b);
+          else if (j == 32) pair<4>(key[i], a, b);
+          else if (j == 64) pair<8>(key[i], a, b);
+          else if (j == 128) pair<16>(key[i], a, b);
+          else pair<32>(key[i], a, b);
+          key[i] = one_of(a, b, side);
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if ((i & j) == 0) {
-            const uint32_t a = key[i], b = key[i | j];
-            const bool up = (((t * 8 + i) & k) == 0);
-            key[i] = up ? min(a, b) : max(a, b);
-            key[i | j] = up ? max(a, b) : min(a, b);
+            const uint32_t a = key[i], b = key[i | j], up = k < 8 ? (i & k ? ~0u : 0u) : turn;
+            key[i] = one_of(a, b, up);
+            key[i | j] = one_of(a, b, ~up);
           }
       }
     }
   }
 }
 
-// The first `chunks` blocks sort kChunk ids each, with their places, by id and then by place (no two keys are alike: there is one order); the others clear the gradient, where it
+// The first `chunks` blocks sort CHUNK ids each, with their places, by id and then by place (no two keys are alike: there is one order); the others clear the gradient, where it
 // is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.  Past the caches: the write-back of
 // plain stores falls into the launches that follow (38.4 MB with 3968 rows of 192: 37 us in all, 34 past them).
-__global__ __launch_bounds__(256) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
+template <int CHUNK>
+__global__ __launch_bounds__(CHUNK / 8) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
                                                          int32_t* __restrict__ pos, uint8_t* __restrict__ clear, size_t head, size_t words, int tail) {
   if (blockIdx.x >= chunks) {
-    const size_t at = (size_t)(blockIdx.x - chunks) * 256 + threadIdx.x, step = (size_t)(gridDim.x - chunks) * 256;
+    const size_t at = (size_t)(blockIdx.x - chunks) * (CHUNK / 8) + threadIdx.x, step = (size_t)(gridDim.x - chunks) * (CHUNK / 8);
     u32x4* body = reinterpret_cast<u32x4*>(clear + head);
     for (size_t i = at; i < words; i += step) __builtin_nontemporal_store(u32x4{0, 0, 0, 0}, body + i);
     if (at < head) clear[at] = 0;
     if (at < (size_t)tail) clear[head + words * 16 + at] = 0;
     return;
   }
-  __shared__ uint32_t lds[kChunk];
-  const int64_t base = (int64_t)blockIdx.x * kChunk;
+  constexpr int kPlace = __builtin_ctz(CHUNK);
+  constexpr uint32_t kLast = (1u << (32 - kPlace)) - 1;
+  __shared__ uint32_t lds[CHUNK];
+  const int64_t base = (int64_t)blockIdx.x * CHUNK;
   uint32_t key[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int at = threadIdx.x * 8 + i;
     const int id = base + at < rows ? ids[base + at] : -1;
-    key[i] = (id >= 0 && id < vocab ? (uint32_t)id : kNone) << 11 | (uint32_t)at;
+    key[i] = (id >= 0 && id < vocab ? (uint32_t)id : kLast) << kPlace | (uint32_t)at;
   }
-  sort_chunk(key, lds);
+  sort_chunk<CHUNK>(key, lds);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t at = base + threadIdx.x * 8 + i;
-    sid[at] = key[i] >> 11, pos[at] = (int32_t)(base + (key[i] & (kChunk - 1)));
+    const uint32_t id = key[i] >> kPlace;
+    sid[at] = id == kLast ? kNone : id, pos[at] = (int32_t)(base + (key[i] & (CHUNK - 1)));
   }
 }
 
@@ -187,6 +230,41 @@ __global__ __launch_bounds__(1024) void embed_merge_kernel(int64_t total, int64_
   if ((threadIdx.x & 3) == 1) pos_out[to] = place;
 }
 
+// Few rows: a wave finds the rows of its own row's token and, for the first of them, adds up 512 columns of all.  128 rows of 2048: 4.8 us, by the sort 12.8.
+template <typename T, typename G, bool ADD, bool TINY>
+__global__ __launch_bounds__(256) void embed_few_kernel(int rows, int vocab, int d, int tiles, const int32_t* __restrict__ ids, const T* __restrict__ dy, float scale,
+                                                        G* __restrict__ dtable) {
+  constexpr int U = 8;
+  static_assert(kFewRows == 128);
+  const int w = blockIdx.x * 4 + (threadIdx.x >> 6), row = w / tiles, lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const int id0 = ids[min(lane, rows - 1)], id1 = ids[min(lane + 64, rows - 1)], id = __builtin_amdgcn_readfirstlane(ids[row]);
+  if (id < 0 || id >= vocab) return;
+  unsigned long long has0 = __ballot(lane < rows && id0 == id), has1 = __ballot(lane + 64 < rows && id1 == id);
+  if (row != (has0 ? __ffsll(has0) - 1 : 63 + __ffsll(has1))) return;
+  const Lane<TINY> own(w % tiles * kCols + lane * 8, d);
+  Loose8<G> old;
+  if constexpr (ADD) own.load(old, dtable + (size_t)id * d);
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  while (has0 | has1) {
+    Loose8<T> raw[U];
+    int n = 0, at = row;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {   // (behind the last row, that again)
+      if (has0 | has1) {
+        at = has0 ? __ffsll(has0) - 1 : 63 + __ffsll(has1);
+        (has0 ? has0 : has1) &= (has0 ? has0 : has1) - 1;
+        n = u + 1;
+      }
+      own.load(raw[u], dy + (size_t)at * d);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < n) add8(raw[u], sum);
+  }
+  finish<G, ADD>(own, sum, old, scale, dtable + (size_t)id * d);
+}
+
 // A wave adds up kCols columns of `piece` rows that follow each other in the order of their tokens.  A token whose rows all lie in the piece is done;
 // of one that goes on in front of or behind it, what lies here is left as a part: parts[2 p] for the first token, parts[2 p + 1] for the last (the first, where there is but
 // one and it goes on in front).  What is added to is requested with the rows, not when their sum is there.  Bound by memory: 32768 rows x 4096 (bf16, to fp32)
@@ -228,16 +306,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece
       if (id[u] == before || !ends) {
         own.store(parts + (size_t)(2 * p + (id[u] == before ? 0 : 1)) * d, sum);
       } else {
-        float x[8];
-        if constexpr (ADD) {
-          old[u].get(x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
-        }
-        own.store(dtable + (size_t)id[u] * d, x);
+        finish<G, ADD>(own, sum, old[ADD ? u : 0], scale, dtable + (size_t)id[u] * d);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] = 0.f;
@@ -291,18 +360,6 @@ __global__ __launch_bounds__(64 * kJoin) void embed_join_kernel(int64_t total, i
       n = (int)from;
     }
   }
-  auto store = [&](uint32_t id, const Loose8<G>& old, float (&sum)[8]) {
-    float x[8];
-    if constexpr (ADD) {
-      old.get(x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = fmaf(scale, sum[j], x[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = scale * sum[j];
-    }
-    own.store(dtable + (size_t)id * d, x);
-  };
   if (lane == 0 && n > kAlone) who = wave, many = n;
   if (n > 0 && n <= kAlone) {
     float sum[8];
@@ -312,7 +369,7 @@ __global__ __launch_bounds__(64 * kJoin) void embed_join_kernel(int64_t total, i
     own.load(begun, parts + (size_t)(2 * p + 1) * d);
     begun.get(sum);
     add_parts(own, parts, p, n, d, sum);
-    store(id, old, sum);
+    finish<G, ADD>(own, sum, old, scale, dtable + (size_t)id * d);
   }
   __syncthreads();
   if (many == 0) return;
@@ -335,19 +392,22 @@ __global__ __launch_bounds__(64 * kJoin) void embed_join_kernel(int64_t total, i
   for (int k = 0; k < kJoin; ++k)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += lds[k][j * 64 + lane];
-  store(id, old, sum);
+  finish<G, ADD>(own, sum, old, scale, dtable + (size_t)id * d);
 }
 
 struct Plan {
   int64_t total, pieces;   // rows up to a whole chunk
-  int piece, tiles;
+  int chunk, piece, tiles;
   size_t ids[2], parts, bytes;
 };
 constexpr int64_t kWaves = 4096;   // waves that the sums are spread over at least, where there are rows for it
 
-Plan make_plan(int64_t rows, int64_t d) {
+Plan make_plan(int64_t rows, int vocab, int64_t d) {
   Plan p;
-  p.total = (rows + kChunk - 1) / kChunk * kChunk;
+  // one block for all rows where it can: no runs are left to join, which takes longer than the larger sort
+  // (4096 rows of 2048: 23 us in place of 26; 8192, sorted by one block: 37 in place of 34)
+  p.chunk = rows > kChunk && rows <= kWhole && vocab < 1 << (32 - __builtin_ctz(kWhole)) ? kWhole : kChunk;
+  p.total = (rows + p.chunk - 1) / p.chunk * p.chunk;
   p.tiles = (int)((d + kCols - 1) / kCols);
   p.piece = 8;
   while (p.piece < 64 && (rows + p.piece - 1) / p.piece * p.tiles > kWaves) p.piece *= 2;
@@ -363,6 +423,12 @@ Plan make_plan(int64_t rows, int64_t d) {
 
 template <typename T, typename G, bool ADD, bool TINY>
 hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const int32_t* pos, float* parts, hipStream_t s) {
+  if (a.rows <= kFewRows) {
+    ProfScope ps("embed_few", (double)a.rows * a.d, (double)a.rows * a.d * sizeof(T), s);
+    hipLaunchKernelGGL((embed_few_kernel<T, G, ADD, TINY>), dim3((unsigned)((a.rows * p.tiles + 3) / 4)), dim3(256), 0, s, (int)a.rows, a.vocab, (int)a.d, p.tiles, a.ids,
+                       (const T*)a.dy, a.scale, (G*)a.dtable);
+    return hipGetLastError();
+  }
   const unsigned blocks = (unsigned)((p.pieces * p.tiles + 3) / 4);
   {
     ProfScope ps("embed_sum", (double)a.rows * a.d, (double)a.rows * a.d * sizeof(T), s);
@@ -406,31 +472,31 @@ hipError_t launch_embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, 
                         : embed_fwd<float>(rows, vocab, d, ids, (const float*)table, scale, (float*)out, s);
 }
 
-size_t embed_bwd_workspace_bytes(int64_t rows, int64_t d) { return make_plan(std::max<int64_t>(rows, 1), d).bytes; }
+size_t embed_bwd_workspace_bytes(int64_t rows, int vocab, int64_t d) { return make_plan(std::max<int64_t>(rows, 1), vocab, d).bytes; }
 
 hipError_t launch_embed_bwd(const EmbedBwdArgs& a, hipStream_t s) {
-  const Plan p = make_plan(std::max<int64_t>(a.rows, 1), a.d);
+  const Plan p = make_plan(std::max<int64_t>(a.rows, 1), a.vocab, a.d);
   char* ws = (char*)a.workspace;
-  const int chunks = a.rows > 0 ? (int)(p.total / kChunk) : 0;
+  const int chunks = a.rows > kFewRows ? (int)(p.total / p.chunk) : 0;
   const size_t bytes = a.accumulate ? 0 : (size_t)a.vocab * (size_t)a.d * dtype_size(a.table_dtype);
   const size_t head = std::min(bytes, (16 - ((uintptr_t)a.dtable & 15)) & 15), words = (bytes - head) / 16;
   const int tail = (int)(bytes - head - words * 16);
-  const int clear = bytes ? (int)std::min<size_t>((words + 1023) / 1024 + 1, 8192) : 0;
+  const int clear = bytes ? (int)std::min<size_t>((words + 1023) / 1024 + 1, 8192 * kChunk / p.chunk) : 0;
   uint32_t* sid[2];
   int32_t* pos[2];
   for (int k = 0; k < 2; ++k) sid[k] = (uint32_t*)(ws + p.ids[k]), pos[k] = (int32_t*)(sid[k] + p.total);
-  if (chunks + clear == 0) return hipSuccess;
-  {
+  if (chunks + clear > 0) {
     ProfScope ps("embed_sort", 0, (double)bytes, s);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(chunks + clear), dim3(256), 0, s, a.rows, a.vocab, chunks, a.ids, sid[0], pos[0], (uint8_t*)a.dtable, head, words, tail);
+    const auto kernel = p.chunk == kWhole ? embed_sort_kernel<kWhole> : embed_sort_kernel<kChunk>;
+    hipLaunchKernelGGL(kernel, dim3(chunks + clear), dim3(p.chunk / 8), 0, s, a.rows, a.vocab, chunks, a.ids, sid[0], pos[0], (uint8_t*)a.dtable, head, words, tail);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (a.rows <= 0) return hipSuccess;
   int at = 0;
-  for (int64_t run = kChunk; run < p.total; run *= kWays, at ^= 1) {
+  for (int64_t run = p.chunk; run < p.total; run *= kWays, at ^= 1) {
     ProfScope ps("embed_merge", 0, 0, s);
     const dim3 grid((unsigned)(p.total / 256)), block(1024);
-    if (run == kChunk) {
+    if (run == kChunk) {   // (whole chunks leave one run)
       const size_t lds = (size_t)std::min<int64_t>(p.total, kChunk * kWays) * sizeof(uint32_t);
       if (const hipError_t e = hipFuncSetAttribute((const void*)embed_merge_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, kChunk * kWays * sizeof(uint32_t))) return e;
       hipLaunchKernelGGL(embed_merge_kernel<true>, grid, block, lds, s, p.total, run, sid[at], pos[at], sid[at ^ 1], pos[at ^ 1]);

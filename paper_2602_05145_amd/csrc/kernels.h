@@ -295,7 +295,7 @@ struct EmbedBwdArgs {
   const int32_t* ids; const void* dy; float scale; void* dtable; int table_dtype, accumulate, dtype;
   void* workspace;
 };
-size_t embed_bwd_workspace_bytes(int64_t rows, int64_t d);
+size_t embed_bwd_workspace_bytes(int64_t rows, int vocab, int64_t d);
 hipError_t launch_embed_bwd(const EmbedBwdArgs& a, hipStream_t s);
 
 // ---- verify.hip --------------------------------------------------------------------------------------

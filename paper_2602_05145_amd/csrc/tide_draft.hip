@@ -1308,7 +1308,7 @@ int tide_embed_fwd(int64_t rows, int32_t vocab, int64_t d, const int32_t* ids, c
 }
 
 size_t tide_embed_bwd_workspace_bytes(int64_t rows, int32_t vocab, int64_t d) {
-  return embed_ok(rows, vocab, d, 1.f, TIDE_DTYPE_FP32) ? embed_bwd_workspace_bytes(rows, d) : 0;
+  return embed_ok(rows, vocab, d, 1.f, TIDE_DTYPE_FP32) ? embed_bwd_workspace_bytes(rows, vocab, d) : 0;
 }
 
 int tide_embed_bwd(int64_t rows, int32_t vocab, int64_t d, const int32_t* ids, const void* dy, float scale, void* dtable, int dtable_dtype, int accumulate, int dtype,
@@ -1320,7 +1320,7 @@ int tide_embed_bwd(int64_t rows, int32_t vocab, int64_t d, const int32_t* ids, c
   if (((uintptr_t)ids & 3) || ((uintptr_t)dy & (size - 1)) || ((uintptr_t)dtable & (size_of_table - 1)))
     return fail(TIDE_ERR_CONFIG, "ids, dy and dtable must be aligned as their elements");
   if (((uintptr_t)workspace) & 255) return fail(TIDE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  const size_t need = embed_bwd_workspace_bytes(rows, d);
+  const size_t need = embed_bwd_workspace_bytes(rows, vocab, d);
   if (workspace_bytes < need) return fail(TIDE_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
   const EmbedBwdArgs a{rows, vocab, d, ids, dy, scale, dtable, dtable_dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, accumulate, dtype == TIDE_DTYPE_BF16 ? kBF16 : kF32, workspace};
   TIDE_HIP(launch_embed_bwd(a, (hipStream_t)stream), "embed backward");

@@ -120,6 +120,22 @@ def test_gradient_of_tokens_over_many_pieces(dtype, out, d, accumulate):
     check_gradient(ids, dtype, out, len(lengths) + 2, d, accumulate, repeat=True)
 
 
+@pytest.mark.parametrize("how", ["frequent", "one", "few", "holes"])
+@pytest.mark.parametrize("rows", [127, 128, 129, 2048, 2049, 4096, 4097, 8191, 8192, 8193])
+def test_gradient_at_the_borders_of_forms(rows, how):
+    check_gradient(make_ids(rows, 300, how, rows), "bf16", "fp32", 300, 72, rows % 2 == 0, repeat=True)
+
+
+@pytest.mark.parametrize("rows", [100, 4096, 8192])
+@pytest.mark.parametrize("vocab", [2 ** 19 - 1, 2 ** 19, 2 ** 20 - 1, 2 ** 20, 2 ** 20 + 1])
+def test_gradient_of_ids_that_fill_their_bits(rows, vocab):
+    ids = make_ids(rows, vocab, "holes", 2)
+    ids[::5] = vocab - 1
+    ids[1::7] = vocab       # no token
+    ids[2::7] = vocab - 2
+    check_gradient(ids, "bf16", "bf16", vocab, 9, False, repeat=True)
+
+
 @pytest.mark.parametrize("rows,others", [(40000, 0), (300000, 0), (300000, 777), (32768, 1)])
 def test_gradient_of_one_token_in_most_rows(rows, others):
     ids = torch.full((rows,), 40, dtype=torch.int32, device=DEV)
