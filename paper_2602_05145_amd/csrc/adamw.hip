@@ -45,15 +45,7 @@ __host__ __device__ __forceinline__ uint32_t step_key(uint32_t seed, int64_t t) 
   return mix(mix(seed ^ (uint32_t)t) + (uint32_t)((uint64_t)t >> 32));
 }
 
-// Four consecutive elements of an array, aligned as one is.  WHOLE: all of them are there; else the first `count`.  ONCE: past the caches.
-template <bool ONCE, typename V> __device__ __forceinline__ auto fetch(const void* p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
-  else return *reinterpret_cast<const V*>(p);
-}
-template <bool ONCE, typename V, typename X> __device__ __forceinline__ void put(void* p, const X& x) {
-  if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<V*>(p));
-  else *reinterpret_cast<V*>(p) = x;
-}
+// Four consecutive elements of an array, aligned as one is.  WHOLE: all of them are there; else the first `count`.
 template <bool WHOLE, bool ONCE>
 struct Four {
   static __device__ __forceinline__ void load(const float* p, int count, float (&x)[4]) {

@@ -12,6 +12,7 @@ constexpr int kCols = 512;        // columns of a wave: eight a lane
 constexpr int kChunk = 2048;      // rows that a block sorts, eight a thread; up to kWhole where one block then sorts all
 constexpr int kWhole = 4096;
 constexpr int kWays = 16;         // sorted runs that a pass joins
+constexpr double kLastCache = 256 << 20;   // bytes that fill it
 constexpr int kFewRows = 128;     // rows of a backward pass without a sort
 constexpr int kJoin = 16;         // pieces that a block joins
 constexpr int kAlone = 16;        // parts of a token that one wave adds up
@@ -26,12 +27,12 @@ template <bool TINY>
 struct Lane {
   int at, skip;
   __device__ __forceinline__ Lane(int c, int d) : at(TINY ? 0 : min(c, d - 8)), skip(TINY ? (c > 0 ? 8 : 8 - d) : min(c - at, 8)) {}
-  template <typename T> __device__ __forceinline__ void load(Loose8<T>& x, const T* row) const {
+  template <bool ONCE = false, typename T> __device__ __forceinline__ void load(Loose8<T>& x, const T* row) const {
     if constexpr (TINY) x.load_some(row, 8 - skip);
-    else x.load(row + at);
+    else x.template load<ONCE>(row + at);
   }
-  template <typename T> __device__ __forceinline__ void store(T* row, const float (&x)[8]) const {
-    if (!TINY && skip == 0) return store_loose8(row + at, x);
+  template <bool ONCE = false, typename T> __device__ __forceinline__ void store(T* row, const float (&x)[8]) const {
+    if (!TINY && skip == 0) return store_loose8<ONCE>(row + at, x);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (TINY ? j < 8 - skip : j >= skip) stf(row, at + j, x[j]);
@@ -60,8 +61,9 @@ __device__ __forceinline__ void finish(const Lane<TINY>& own, const float (&sum)
 }
 
 // One wave copies G * kCols columns of R rows that follow each other, all of its loads under way together: 32665 rows of 232 columns with a wave for each four in 7.6 us, for each
-// one 9.1.
-template <typename T, int G, int R, bool TINY>
+// one 9.1.  ONCE: past the caches, for what they cannot hold anyway: 32768 x 4096 (bf16) 67 -> 60 us and 402 -> 387 with a sum that reads it; fp32, 32768 x 2048: 84 -> 94 and
+// 414 -> 399.
+template <typename T, int G, int R, bool TINY, bool ONCE = false>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(int64_t rows, int vocab, int d, int tiles, const int32_t* __restrict__ ids, const T* __restrict__ table,
                                                         float scale, T* __restrict__ out) {
   const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -87,7 +89,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(int64_t rows, int vocab,
       raw[r][g].get(x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = some[r] ? x[j] * scale : 0.f;
-      Lane<TINY>(c + g * kCols, d).store(out + (size_t)(row + r) * d, x);
+      Lane<TINY>(c + g * kCols, d).template store<ONCE>(out + (size_t)(row + r) * d, x);
     }
   }
 }
@@ -152,8 +154,9 @@ __device__ __forceinline__ void sort_chunk(uint32_t (&key)[8], uint32_t* lds) {
 }
 
 // The first `chunks` blocks sort CHUNK ids each, with their places, by id and then by place (no two keys are alike: there is one order); the others clear the gradient, where it
-// is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.  Past the caches: the write-back of
-// plain stores falls into the launches that follow (38.4 MB with 3968 rows of 192: 37 us in all, 34 past them).
+// is written and not added to, while they do: `head` bytes up to a multiple of 16, `words` of 16, `tail` bytes.  One store a
+// thread, as far as a launch's blocks reach: 131 MB in 20 us and 525 in 80, where 8192 blocks in a loop take 22 and 107.  Past the caches: the write-back of plain stores
+// falls into the launches that follow.
 template <int CHUNK>
 __global__ __launch_bounds__(CHUNK / 8) void embed_sort_kernel(int64_t rows, int vocab, int chunks, const int32_t* __restrict__ ids, uint32_t* __restrict__ sid,
                                                          int32_t* __restrict__ pos, uint8_t* __restrict__ clear, size_t head, size_t words, int tail) {
@@ -459,6 +462,7 @@ hipError_t embed_fwd(int64_t rows, int vocab, int d, const int32_t* ids, const T
   if (d < 8) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 1, true>), grid, block, 0, s, rows, vocab, d, 1, ids, table, scale, out);
   else if (few) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 1, false>), grid, block, 0, s, rows, vocab, d, tiles, ids, table, scale, out);
   else if (narrow) hipLaunchKernelGGL((embed_fwd_kernel<T, 1, 4, false>), grid, block, 0, s, rows, vocab, d, 1, ids, table, scale, out);
+  else if ((double)rows * d * sizeof(T) >= kLastCache) hipLaunchKernelGGL((embed_fwd_kernel<T, 4, 1, false, true>), grid, block, 0, s, rows, vocab, d, tiles, ids, table, scale, out);
   else hipLaunchKernelGGL((embed_fwd_kernel<T, 4, 1, false>), grid, block, 0, s, rows, vocab, d, tiles, ids, table, scale, out);
   return hipGetLastError();
 }
@@ -481,7 +485,7 @@ hipError_t launch_embed_bwd(const EmbedBwdArgs& a, hipStream_t s) {
   const size_t bytes = a.accumulate ? 0 : (size_t)a.vocab * (size_t)a.d * dtype_size(a.table_dtype);
   const size_t head = std::min(bytes, (16 - ((uintptr_t)a.dtable & 15)) & 15), words = (bytes - head) / 16;
   const int tail = (int)(bytes - head - words * 16);
-  const int clear = bytes ? (int)std::min<size_t>((words + 1023) / 1024 + 1, 8192 * kChunk / p.chunk) : 0;
+  const int clear = bytes ? (int)std::min<size_t>(words / (p.chunk / 8) + 1, 1 << 22) : 0;
   uint32_t* sid[2];
   int32_t* pos[2];
   for (int k = 0; k < 2; ++k) sid[k] = (uint32_t*)(ws + p.ids[k]), pos[k] = (int32_t*)(sid[k] + p.total);

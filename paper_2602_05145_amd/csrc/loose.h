@@ -14,11 +14,21 @@ typedef u32x2 __attribute__((aligned(2))) u32x2_of_halves;
 typedef u32x2 __attribute__((aligned(1))) u32x2_of_bytes;
 typedef uint32_t __attribute__((aligned(1))) u32_of_bytes;
 
+// ONCE: past the caches.
+template <bool ONCE, typename V> __device__ __forceinline__ auto fetch(const void* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+template <bool ONCE, typename V, typename X> __device__ __forceinline__ void put(void* p, const X& x) {
+  if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<V*>(p));
+  else *reinterpret_cast<V*>(p) = x;
+}
+
 // Eight consecutive elements as loaded
 template <typename T> struct Loose8;
 template <> struct Loose8<bf16_t> {
   u32x4 a;
-  __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const u32x4_of_halves*>(p); }
+  template <bool ONCE = false> __device__ __forceinline__ void load(const bf16_t* p) { a = fetch<ONCE, u32x4_of_halves>(p); }
   __device__ __forceinline__ void load_some(const bf16_t* p, int count) {   // the first `count`, zeros behind them
     a = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -32,7 +42,7 @@ template <> struct Loose8<bf16_t> {
 };
 template <> struct Loose8<float> {
   f32x4 a, b;
-  __device__ __forceinline__ void load(const float* p) { a = reinterpret_cast<const f32x4_of_floats*>(p)[0], b = reinterpret_cast<const f32x4_of_floats*>(p)[1]; }
+  template <bool ONCE = false> __device__ __forceinline__ void load(const float* p) { a = fetch<ONCE, f32x4_of_floats>(p), b = fetch<ONCE, f32x4_of_floats>(p + 4); }
   __device__ __forceinline__ void load_some(const float* p, int count) {
     a = b = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -46,12 +56,12 @@ template <> struct Loose8<float> {
     for (int j = 0; j < 4; ++j) x[j] = a[j], x[4 + j] = b[j];
   }
 };
-__device__ __forceinline__ void store_loose8(float* p, const float (&x)[8]) {
-  reinterpret_cast<f32x4_of_floats*>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-  reinterpret_cast<f32x4_of_floats*>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+template <bool ONCE = false> __device__ __forceinline__ void store_loose8(float* p, const float (&x)[8]) {
+  put<ONCE, f32x4_of_floats>(p, f32x4{x[0], x[1], x[2], x[3]});
+  put<ONCE, f32x4_of_floats>(p + 4, f32x4{x[4], x[5], x[6], x[7]});
 }
-__device__ __forceinline__ void store_loose8(bf16_t* p, const float (&x)[8]) {
-  *reinterpret_cast<u32x4_of_halves*>(p) = u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])};
+template <bool ONCE = false> __device__ __forceinline__ void store_loose8(bf16_t* p, const float (&x)[8]) {
+  put<ONCE, u32x4_of_halves>(p, u32x4{f2bf2(x[0], x[1]), f2bf2(x[2], x[3]), f2bf2(x[4], x[5]), f2bf2(x[6], x[7])});
 }
 
 }  // namespace tide

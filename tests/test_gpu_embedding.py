@@ -50,6 +50,23 @@ def test_lookup(rows, vocab, d, off, dtype):
     table.check()
 
 
+@pytest.mark.parametrize("dtype,rows,d,off", [("bf16", 32768, 4096, 0), ("bf16", 33001, 4107, 1), ("fp32", 16385, 4101, 3)])
+def test_lookup_of_more_than_the_last_cache(dtype, rows, d, off):
+    vocab = 5000
+    ids = make_ids(rows, vocab, "holes", 8)
+    table = torch.randn(vocab, d, device=DEV, generator=gen(9)).to(TDT[dtype])
+    out = Loose(rows * d, TDT[dtype], off)
+    B.tide_embed_fwd(rows, vocab, d, ids, table, 1.7, out.t, CODE[dtype], stream())
+    s = torch.tensor(1.7, dtype=torch.float32, device=DEV)
+    got = out.t.view(rows, d)
+    for a in range(0, rows, 4096):
+        some = ids[a:a + 4096]
+        fine = (some >= 0) & (some < vocab)
+        want = torch.where(fine[:, None], table[some.clamp(0, vocab - 1).long()].float() * s, 0.0).to(TDT[dtype])
+        assert torch.equal(got[a:a + 4096], want)
+    out.check()
+
+
 def gradient(ids, dy, scale, vocab, start, accumulate):
     """The definition in 64 bits, and the sums of magnitudes and the numbers of rows that bound what 32 bits may be off."""
     d = dy.shape[1]
