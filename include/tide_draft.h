@@ -553,7 +553,7 @@ int tide_adamw_dev(int32_t n_tensors, const tide_adamw_tensor *tensors, const fl
  * -inf is a column without probability.  A target row that holds NaN or +inf or nothing above -inf has no distribution: a token there is refused and -1 is
  * emitted (also where temperature[b] is negative, infinite or NaN).  A draft row of that kind: the token is refused and the target's p_j stands alone, as it does where
  * max(0, p_j - q_j) is 0 everywhere.  Exponentials and sums are in 64 bits.
- * 0 <= n_requests <= rows <= 2^20, vocab <= 2^28, rows * vocab <= 2^35.  Enqueues four or five kernels and nothing else. */
+ * 0 <= n_requests <= rows <= 2^20, vocab <= 2^28, rows * vocab <= 2^35.  Enqueues three or five kernels and nothing else. */
 size_t tide_verify_workspace_bytes(int64_t rows, int32_t n_requests, int32_t vocab);
 int tide_verify_drafts(int64_t rows, int32_t n_requests, int32_t vocab, const int32_t *cu_rows, const void *target, int64_t ldt,
                        const void *draft, int64_t ldd, const int32_t *draft_tokens, const float *temperature,

@@ -350,21 +350,20 @@ __device__ __forceinline__ double block_sum(double v, double* red) {   // every 
   return all;
 }
 
-// One block a request.  With rough sums (not `exact`) a comparison next to its border is made again with the sums of its rows in 64 bits.
-template <typename T>
-__global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, int parts, int picks, bool exact, const Part* __restrict__ stats, Sums* __restrict__ sums,
-                                                            Draw* __restrict__ draws) {
+// What a request emits, by one block, which `writes` it; whether a token remains to be drawn, and from what.  With sums in 32 bits (not EXACT) a comparison next to its border
+// is made again with the sums of its rows in 64 bits.
+template <typename T, int WAVES, bool EXACT>
+__device__ __forceinline__ bool decide(const VerifyArgs& a, int b, int parts, const Part* __restrict__ stats, bool writes, Draw& draw, Sums& of) {
   constexpr int kAhead = 32;   // drafted positions that are looked at together
   __shared__ Row of_p[kAhead + 1], of_q[kAhead];
   __shared__ int stop_s, token_s, unsure_s;
-  __shared__ double red[8];
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ double red[WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t V = a.V;
   const View v = view_of(a.cu, b, a.rows, a.rows - a.requests);
-  if (threadIdx.x == 0) draws[b].p = -1;
   if (!v.any) {
-    if (threadIdx.x == 0) a.accepted[b] = 0;
-    return;
+    if (writes && threadIdx.x == 0) a.accepted[b] = 0;
+    return false;
   }
   const float tau = tau_of(a.temperature, b);
   const bool sampled = tau > 0.f, drawn = sampled && a.draft;
@@ -376,7 +375,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
   auto whole = [&](const T* row, float top) {   // the sum of a row in 64 bits, by the block
     const Scale e(c, top);
     double sum = 0.0;
-    for (int64_t col = threadIdx.x * 8; col < V; col += 512 * 8) {
+    for (int64_t col = threadIdx.x * 8; col < V; col += WAVES * 512) {
       Eight<T> raw;
       float z[8];
       raw.load(row, col, V);
@@ -384,7 +383,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum += e.of(z[k]);
     }
-    return block_sum<8>(sum, red);
+    return block_sum<WAVES>(sum, red);
   };
   // a token is accepted if u q(x) < p(x); one that is no token ends the draft
   int j = 0, i0 = 0, taken = -1;
@@ -403,7 +402,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
           if (drawn) zq = ldf(z_draft, (size_t)(i * a.ldd + x));
         }
       }
-      for (int t = wave; t < tasks; t += 8) {
+      for (int t = wave; t < tasks; t += WAVES) {
         const bool of_other = t >= rows;
         const int k = of_other ? t - rows : t;
         const Row r = join_row((of_other ? of_draft : of_target) + (int64_t)(i0 + k) * parts, parts, c, sampled, lane);
@@ -425,7 +424,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
               if (drawn) qx = of_q[lane].ok ? Scale(c, of_q[lane].top).of(zq) / of_q[lane].sum : __builtin_nan("");
               const double left = (double)u * qx;
               takes = left < px;
-              unsure = !exact && lane >= sure && (rough_ok(tau) ? fabs(left - px) <= kNear * px : left == left);
+              unsure = !EXACT && lane >= sure && (rough_ok(tau) ? fabs(left - px) <= kNear * px : left == left);
             }
           }
           const unsigned long long not_taken = __ballot(lane < n && (!takes || unsure));
@@ -437,7 +436,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
           }
         }
         __syncthreads();
-        again = unsure_s;
+        again = !EXACT && unsure_s;
         if (again) {
           const int k = stop_s;
           const double sp = whole(z_target + (int64_t)(i0 + k) * a.ldt, of_p[k].top);
@@ -461,19 +460,27 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
   if (tau == tau) p = of_p[j - i0];
   if (drawn && refused) q = of_q[j - i0];
   const bool told = !sampled || !p.ok;   // the emitted token is known, or there is none
-  for (int64_t i = threadIdx.x; i <= v.n; i += 512)
-    if (i != j || told) a.out[v.row0 + i] = i < j ? a.tokens[v.first + i] : i == j && p.ok ? p.at : -1;
-  if (threadIdx.x == 0) a.accepted[b] = j;
-  if (told) return;
-  if (threadIdx.x == 0) {
-    // (named and not drawn: the token itself is taken off)
-    draws[b] = Draw{v.row0 + j, q.ok ? v.first + j : -1, p.top, q.top, refused && !a.draft ? taken : -1, (int)(v.row0 + j), p.sum, c, -1200.0 / c, a.uniforms[v.row0 + v.n]};
+  if (writes) {
+    for (int64_t i = threadIdx.x; i <= v.n; i += 64 * WAVES)
+      if (i != j || told) a.out[v.row0 + i] = i < j ? a.tokens[v.first + i] : i == j && p.ok ? p.at : -1;
+    if (threadIdx.x == 0) a.accepted[b] = j;
   }
-  if (exact && threadIdx.x < picks) {
-    Sums* s = sums + (int64_t)b * kMaxPicks + threadIdx.x;
-    s->p = threadIdx.x == 0 ? p.sum : 0.0;
-    s->q = threadIdx.x == 0 && q.ok ? q.sum : 0.0;
-  }
+  if (told) return false;
+  // (named and not drawn: the token itself is taken off)
+  draw = Draw{v.row0 + j, q.ok ? v.first + j : -1, p.top, q.top, refused && !a.draft ? taken : -1, (int)(v.row0 + j), p.sum, c, -1200.0 / c, a.uniforms[v.row0 + v.n]};
+  of = Sums{p.sum, q.ok ? q.sum : 0.0};
+  return true;
+}
+
+// One block a request, with sums in 32 bits.
+template <typename T>
+__global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, int parts, const Part* __restrict__ stats, Draw* __restrict__ draws) {
+  const int b = blockIdx.x;
+  Draw d;
+  Sums of;
+  const bool drawn = decide<T, 8, false>(a, b, parts, stats, true, d, of);
+  if (!drawn) d.p = -1;
+  if (threadIdx.x == 0) draws[b] = d;
 }
 
 // What a request's token is drawn from, as the last three kernels go over it.
@@ -563,32 +570,56 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a, in
   }
 }
 
-// A wave weighs units: the 512 columns that it takes of each step, or `per` steps of them.
+// A wave weighs units: the 512 columns that it takes of each step, or `per` steps of them.  `x` holds what the first of them loads.
 template <typename T>
-__global__ __launch_bounds__(256) void verify_weights_kernel(const VerifyArgs a, int picks, int64_t span, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
-                                                             double* __restrict__ weights) {
-  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const Draw d = draws[b];
-  if (d.p < 0) return;
-  Source<T> s(a, d);
-  const int64_t unit = (int64_t)per * 512, to = min((pick + 1) * span, a.V);
-  typename Source<T>::Columns x;
-  s.load(pick * span + wave * unit + lane * 8, x);   // (under way while the sums are joined)
-  s.join(sums + (int64_t)b * kMaxPicks, picks, lane);
-  for (int64_t first = pick * span + wave * unit; first < to; first += 4 * unit) {
+__device__ __forceinline__ void weigh_units(const Source<T>& s, typename Source<T>::Columns& x, int pick, int64_t span, int per, double* __restrict__ weights) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)per * 512, to = min((pick + 1) * span, s.V), begin = pick * span + (threadIdx.x >> 6) * unit;
+  for (int64_t first = begin; first < to; first += 4 * unit) {
     double sum = 0.0;
     const int64_t end = min(first + unit, to);
     for (int64_t base = first; base < end; base += 512) {
-      if (base > pick * span + wave * unit) s.load(base + lane * 8, x);
+      if (base > begin) s.load(base + lane * 8, x);
       double w[8];
       s.weigh(base + lane * 8, x, w);
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum += w[k];
     }
     sum = wave_sum(sum);
-    if (lane == 0) weights[(int64_t)b * kMaxUnits + first / unit] = sum;
+    if (lane == 0) weights[first / unit] = sum;
   }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void verify_weights_kernel(const VerifyArgs a, int picks, int64_t span, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
+                                                             double* __restrict__ weights) {
+  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
+  const Draw d = draws[b];
+  if (d.p < 0) return;
+  Source<T> s(a, d);
+  typename Source<T>::Columns x;
+  s.load(pick * span + (threadIdx.x >> 6) * (int64_t)per * 512 + (threadIdx.x & 63) * 8, x);   // (under way while the sums are joined)
+  s.join(sums + (int64_t)b * kMaxPicks, picks, threadIdx.x & 63);
+  weigh_units(s, x, pick, span, per, weights + (int64_t)b * kMaxUnits);
+}
+
+// With sums in 64 bits: every block that weighs a part decides by itself what it is a part of, and the first of a request writes that down.  A launch less: a request of 4 + 3 rows of
+// 32000 in 14.9 us, 17.9 with it; 256 requests of 11 x 4096 24.2, 26.1.
+template <typename T>
+__global__ __launch_bounds__(256) void verify_decide_weights_kernel(const VerifyArgs a, int parts, int picks, int64_t span, int per, const Part* __restrict__ stats,
+                                                                    Sums* __restrict__ sums, Draw* __restrict__ draws, double* __restrict__ weights) {
+  const int b = blockIdx.x / picks, pick = blockIdx.x % picks;
+  Draw d;
+  Sums of;
+  const bool drawn = decide<T, 4, true>(a, b, parts, stats, pick == 0, d, of);
+  if (!drawn) d.p = -1;
+  if (pick == 0 && threadIdx.x == 0) draws[b] = d;
+  if (!drawn) return;
+  if (pick == 0 && threadIdx.x < picks) sums[(int64_t)b * kMaxPicks + threadIdx.x] = threadIdx.x == 0 ? of : Sums{0.0, 0.0};
+  Source<T> s(a, d);
+  if (s.zq) s.ip = 1.0 / of.p, s.iq = 1.0 / of.q;
+  typename Source<T>::Columns x;
+  s.load(pick * span + (threadIdx.x >> 6) * (int64_t)per * 512 + (threadIdx.x & 63) * 8, x);
+  weigh_units(s, x, pick, span, per, weights + (int64_t)b * kMaxUnits);
 }
 
 // One wave a request: the first unit whose cumulated weight goes over the border (none: the last that weighs anything), and in it the first column.
@@ -659,7 +690,7 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a, int
 
 int64_t parts_of(int64_t V, int u) { return (V + (int64_t)u * kStep - 1) / ((int64_t)u * kStep); }
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-// Up to so many columns in all rows the exact sums are made at once, which saves a launch: 5M 20.7 us beside 23.8 with sums in 32 bits first, 11M 27.1 / 29.5, 18M 34.8 / 30.4,
+// Up to so many columns in all rows the exact sums are made at once, which saves two launches: 14M take 31 us and 32 with sums in 32 bits first, 18M 35 / 30, 20M 40 / 27,
 // 295M 304 / 178 (bf16).
 constexpr int64_t kFewColumns = 12 << 20;
 
@@ -692,27 +723,29 @@ static hipError_t verify(const VerifyArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((verify_stats_kernel<T, 1>), grid, block, 0, s, a, (int)parts, stats);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  // 4096 blocks (a full batch of 256 x 128256: 200 us; 2048: 211, 8192: 203, 16384: 216), and no part below one step; of each block's four waves every one has whole units
+  // exact: 512 blocks, as each decides (16 requests of up to 5 + 4 rows of 128256: 25.4 us; 256: 27.5, 1024: 27.0); else 4096 (a full batch of 256 x 128256: 200 us;
+  // 2048: 211, 8192: 203, 16384: 216), and no part below one step; of each block's four waves every one has whole units
   const int per = (int)((a.V + 512 * kMaxUnits - 1) / (512 * kMaxUnits));
   const int64_t group = (int64_t)per * kStep, groups = (a.V + group - 1) / group;
-  const int64_t wanted = std::min<int64_t>({groups, kMaxPicks, std::max<int64_t>(1, 4096 / a.requests)});
+  const int64_t wanted = std::min<int64_t>({groups, kMaxPicks, std::max<int64_t>(1, (exact ? 512 : 4096) / a.requests)});
   const int64_t span = (groups + wanted - 1) / wanted * group;
   const int picks = (int)((a.V + span - 1) / span), pieces = (int)((a.V + (int64_t)per * 512 - 1) / ((int64_t)per * 512));
   const dim3 each((unsigned)a.requests), all((unsigned)((int64_t)a.requests * picks));
   const double row = (double)a.requests * a.V * sizeof(T) * (a.draft ? 2 : 1);
-  {
-    ProfScope ps("verify_decide", 0, 0, s);
-    hipLaunchKernelGGL(verify_decide_kernel<T>, each, dim3(512), 0, s, a, (int)parts, picks, exact, stats, sums, draws);
-    if (const hipError_t e = hipGetLastError()) return e;
-  }
   if (!exact) {
+    {
+      ProfScope ps("verify_decide", 0, 0, s);
+      hipLaunchKernelGGL(verify_decide_kernel<T>, each, dim3(512), 0, s, a, (int)parts, stats, draws);
+      if (const hipError_t e = hipGetLastError()) return e;
+    }
     ProfScope ps("verify_sums", 0, row, s);
     hipLaunchKernelGGL(verify_sums_kernel<T>, all, dim3(256), 0, s, a, picks, span, draws, sums);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   {
     ProfScope ps("verify_weights", 0, row, s);
-    hipLaunchKernelGGL(verify_weights_kernel<T>, all, dim3(256), 0, s, a, picks, span, per, draws, sums, weights);
+    if (exact) hipLaunchKernelGGL(verify_decide_weights_kernel<T>, all, dim3(256), 0, s, a, (int)parts, picks, span, per, stats, sums, draws, weights);
+    else hipLaunchKernelGGL(verify_weights_kernel<T>, all, dim3(256), 0, s, a, picks, span, per, draws, sums, weights);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   ProfScope ps("verify_pick", 0, 0, s);
