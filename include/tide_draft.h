@@ -547,7 +547,7 @@ int tide_adamw_dev(int32_t n_tensors, const tide_adamw_tensor *tensors, const fl
  *   draft_tokens DEVICE int32 [rows - n_requests] (may be NULL if that is 0).  One outside [0, vocab) ends its request's draft there: n_b is smaller
  *   temperature  DEVICE float [n_requests], or NULL: 1
  *   uniforms     DEVICE float [rows], in [0, 1)
- *   accepted     DEVICE int32 [n_requests], tokens DEVICE int32 [rows]
+ *   accepted     DEVICE int32 [n_requests], tokens DEVICE int32 [rows]; they overlap none of the others
  *   workspace    DEVICE, 256-byte aligned, of at least tide_verify_workspace_bytes(rows, n_requests, vocab) bytes (0 = sizes the call refuses, or no rows); nothing in it
  *                has to survive between calls, and calls that overlap need one each
  * -inf is a column without probability.  A target row that holds NaN or +inf or nothing above -inf has no distribution: a token there is refused and -1 is
