@@ -229,7 +229,7 @@ __device__ __forceinline__ void work(const Entry& t, const Step& s, int64_t base
 }
 
 // Block b works on 1024 elements of the tensor its index falls in.  Bound by memory.  Past the caches (both ways) where a launch moves more than they hold: the small draft of
-// 216M weights, 32 bits, 702 -> 674 us (5.6 TB/s), the large one of 794M, 8 bits, 2750 -> 2555; 2M weights, which the last cache holds, 10.2 -> 11.2.
+// 125M weights, 32 bits, 702 -> 674 us (5.6 TB/s), the large one of 794M, 8 bits, 2750 -> 2555 (now 644 and 2381: 5.8 and 6.0 TB/s); 2M weights, which the last cache holds, 10.2 -> 11.2.
 template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void adamw_list_kernel(const Table a) {
 #pragma clang fp contract(off)

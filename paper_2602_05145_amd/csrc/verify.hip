@@ -152,7 +152,8 @@ __device__ __forceinline__ int owner_of(const VerifyArgs& a, int64_t row, bool o
 // make a difference have |t| <= 28 and so 2^-18.6.  A thread adds 16 sums of eight, each moved to a new maximum at most as often: 2^-19.  At the ends of fp32 c itself loses bits.
 __device__ __forceinline__ bool rough_ok(float tau) { return tau >= 0x1p-100f && tau <= 0x1p100f; }
 
-// Of U * 2048 columns of one row: the largest value and the sum of exponentials beside it, in 64 bits.
+// Of U * 2048 columns of one row: the largest value and the sum of exponentials beside it, in 64 bits.  Bound by the exponentials: 16 requests of up to 5 + 4 rows of 128256 in 12 us
+// (1.8 TB/s).
 template <typename T, int U>
 __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyArgs a, int parts, Part* __restrict__ stats) {
   __shared__ double sums[4];
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyArgs a, i
   }
 }
 
-// The same in 32 bits, of `columns` columns.
+// The same in 32 bits, of `columns` columns.  Bound by memory, the vector unit as busy: 2816 rows of 128256 (bf16) in 109 us, 6.6 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void verify_rough_stats_kernel(const VerifyArgs a, int parts, int columns, Part* __restrict__ stats) {
   __shared__ Online joined[4];
@@ -472,7 +473,7 @@ __device__ __forceinline__ bool decide(const VerifyArgs& a, int b, int parts, co
   return true;
 }
 
-// One block a request, with sums in 32 bits.
+// One block a request, with sums in 32 bits.  Latency, 5 to 6 us: parts, the walk, the draw's description.
 template <typename T>
 __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, int parts, const Part* __restrict__ stats, Draw* __restrict__ draws) {
   const int b = blockIdx.x;
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(512) void verify_decide_kernel(const VerifyArgs a, 
   if (threadIdx.x == 0) draws[b] = d;
 }
 
-// What a request's token is drawn from, as the last three kernels go over it.
+// What a request's token is drawn from, as the kernels behind go over it.
 template <typename T>
 struct Source {
   const T *zp, *zq;   // zq: NULL where nothing is taken off
@@ -531,6 +532,7 @@ struct Source {
   }
 };
 
+// Sums in 64 bits of the rows that tokens are drawn from.  Bound by the exponentials: 256 requests x 2 rows of 128256 in 27 us, the vector unit 81 % busy.
 template <typename T>
 __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a, int picks, int64_t span, const Draw* __restrict__ draws, Sums* __restrict__ sums) {
   __shared__ double red[8];
@@ -589,6 +591,7 @@ __device__ __forceinline__ void weigh_units(const Source<T>& s, typename Source<
     if (lane == 0) weights[first / unit] = sum;
   }
 }
+// Bound by the same: 256 requests in 50 us, 94 % busy.
 template <typename T>
 __global__ __launch_bounds__(256) void verify_weights_kernel(const VerifyArgs a, int picks, int64_t span, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
                                                              double* __restrict__ weights) {
@@ -622,7 +625,7 @@ __global__ __launch_bounds__(256) void verify_decide_weights_kernel(const Verify
   weigh_units(s, x, pick, span, per, weights + (int64_t)b * kMaxUnits);
 }
 
-// One wave a request: the first unit whose cumulated weight goes over the border (none: the last that weighs anything), and in it the first column.
+// One wave a request: the first unit whose cumulated weight goes over the border (none: the last that weighs anything), and in it the first column.  Latency, 3.4 to 5 us.
 template <typename T>
 __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a, int picks, int units, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
                                                          const double* __restrict__ weights) {
