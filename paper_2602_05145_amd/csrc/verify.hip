@@ -33,6 +33,7 @@ struct Draw { int64_t p, q; float top_p, top_q; int taken, to; double sum, c, le
 
 // 2^(c d) for -1200 <= c d <= 0.  The product rounded to an integer n is what the first step leaves in the low bits of k; on the rest f in [-1/2, 1/2] stands the polynomial
 // 1 + f r(f) of least relative error (8.1e-13) with seven degrees in r, by exchange of its extreme points.  d = 0 gives 1.
+template <bool NORMAL>
 __device__ __forceinline__ double power(double d, double c) {
   constexpr double kShift = 0x1.8p52;
   const double k = fma(d, c, kShift), f = fma(d, c, kShift - k);
@@ -44,15 +45,17 @@ __device__ __forceinline__ double power(double d, double c) {
   r = fma(r, f, 0.05550410935266197);
   r = fma(r, f, 0.2402265069811059);
   r = fma(r, f, 0.6931471805482124);
-  return ldexp(fma(r, f, 1.0), __double2loint(k));
+  const double m = fma(r, f, 1.0);
+  if constexpr (!NORMAL) return ldexp(m, __double2loint(k));
+  return __hiloint2double(__double2hiint(m) + (int)((uint32_t)__double2loint(k) << 20), __double2loint(m));
 }
 // exp((z - top) / tau), c = log2(e) / tau: the difference comes first, so that the largest value gives 1 whatever it is.
 struct Scale {
   double c, top, least;
   __device__ __forceinline__ Scale(double c_, float top_) : Scale(c_, top_, -1200.0 / c_) {}
   __device__ __forceinline__ Scale(double c_, float top_, double least_) : c(c_), top((double)top_), least(least_) {}
-  __device__ __forceinline__ double of(float z) const { return power(fmax((double)z - top, least), c); }     // z <= top, or -inf
-  __device__ __forceinline__ double near(float z) const { return power((double)z - top, c); }                // where -1000 <= c (z - top); a NaN stays
+  __device__ __forceinline__ double of(float z) const { return power<false>(fmax((double)z - top, least), c); }     // z <= top, or -inf
+  __device__ __forceinline__ double near(float z) const { return power<true>((double)z - top, c); }                // where -1000 <= c (z - top); a NaN stays
 };
 __device__ __forceinline__ bool usable(float top) { return fabsf(top) < INFINITY; }   // (a NaN is not)
 
@@ -489,24 +492,23 @@ template <typename T>
 struct Source {
   const T *zp, *zq;   // zq: NULL where nothing is taken off
   Scale ep, eq;
-  double ip, iq;      // 1 / the whole sums; without a draft's row 1, as weights are on any scale
+  double ratio;       // of the whole sums, p's over q's: weights are on the scale of p's exponentials
   int taken;
   int64_t V;
   __device__ __forceinline__ Source(const VerifyArgs& a, const Draw& d)
       : zp((const T*)a.target + d.p * a.ldt), zq(d.q >= 0 ? (const T*)a.draft + d.q * a.ldd : nullptr), ep(d.c, d.top_p, d.least),
-        eq(d.c, d.top_q, d.least), ip(1.0), iq(0.0), taken(d.taken), V(a.V) {}
+        eq(d.c, d.top_q, d.least), ratio(0.0), taken(d.taken), V(a.V) {}
   __device__ __forceinline__ void join(const Sums* s, int picks, int lane) {   // by every wave
     if (!zq) return;
     const Sums mine = lane < picks ? s[lane] : Sums{0.0, 0.0};
-    ip = 1.0 / wave_sum(mine.p), iq = 1.0 / wave_sum(mine.q);
+    ratio = wave_sum(mine.p) / wave_sum(mine.q);
   }
   struct Columns { Eight<T> p, q; };
   __device__ __forceinline__ void load(int64_t col, Columns& x) const {
     x.p.load(zp, col, V);
     if (zq) x.q.load(zq, col, V);
   }
-  __device__ __forceinline__ void weigh(int64_t col, Columns& x, double (&w)[8]) const {   // by a whole wave
-#pragma clang fp contract(off)   // (equal probabilities leave nothing)
+  __device__ __forceinline__ void weigh(int64_t col, Columns& x, double (&w)[8]) const {   // by a whole wave; equal rows leave exactly nothing
     float z[8], y[8];
     x.p.get(col, V, z);
     if (all_near(ep, z)) {
@@ -520,10 +522,10 @@ struct Source {
       x.q.get(col, V, y);
       if (all_near(eq, y)) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = fmax(w[k] * ip - eq.near(y[k]) * iq, 0.0);
+        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.near(y[k]), ratio, w[k]), 0.0);
       } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = fmax(w[k] * ip - eq.of(y[k]) * iq, 0.0);
+        for (int k = 0; k < 8; ++k) w[k] = fmax(fma(-eq.of(y[k]), ratio, w[k]), 0.0);
       }
     } else if (__ballot(taken >= col && taken < col + 8)) {
 #pragma unroll
@@ -575,23 +577,26 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a, in
 // A wave weighs units: the 512 columns that it takes of each step, or `per` steps of them.  `x` holds what the first of them loads.
 template <typename T>
 __device__ __forceinline__ void weigh_units(const Source<T>& s, typename Source<T>::Columns& x, int pick, int64_t span, int per, double* __restrict__ weights) {
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)per * 512, to = min((pick + 1) * span, s.V), begin = pick * span + (threadIdx.x >> 6) * unit;
-  for (int64_t first = begin; first < to; first += 4 * unit) {
+  const int lane = threadIdx.x & 63, steps = (int)(span / 512), own = (int)(threadIdx.x >> 6) * per;   // (in steps of 512 columns)
+  const int64_t begin = pick * span;
+  weights += (int64_t)pick * (steps / per) + (threadIdx.x >> 6);
+  const int to = (int)min((int64_t)steps, (s.V - begin + 511) / 512);
+  for (int first = own; first < to; first += 4 * per, weights += 4) {
     double sum = 0.0;
-    const int64_t end = min(first + unit, to);
-    for (int64_t base = first; base < end; base += 512) {
-      if (base > begin) s.load(base + lane * 8, x);
+    const int end = min(first + per, to);
+    for (int step = first; step < end; ++step) {
+      const int64_t col = begin + step * 512 + lane * 8;
+      if (step > own) s.load(col, x);
       double w[8];
-      s.weigh(base + lane * 8, x, w);
+      s.weigh(col, x, w);
 #pragma unroll
       for (int k = 0; k < 8; ++k) sum += w[k];
     }
     sum = wave_sum(sum);
-    if (lane == 0) weights[first / unit] = sum;
+    if (lane == 0) *weights = sum;
   }
 }
-// Bound by the same: 256 requests in 50 us, 94 % busy.
+// Bound by the same: 256 requests in 43 us, 94 % busy.
 template <typename T>
 __global__ __launch_bounds__(256) void verify_weights_kernel(const VerifyArgs a, int picks, int64_t span, int per, const Draw* __restrict__ draws, const Sums* __restrict__ sums,
                                                              double* __restrict__ weights) {
@@ -619,7 +624,7 @@ __global__ __launch_bounds__(256) void verify_decide_weights_kernel(const Verify
   if (!drawn) return;
   if (pick == 0 && threadIdx.x < picks) sums[(int64_t)b * kMaxPicks + threadIdx.x] = threadIdx.x == 0 ? of : Sums{0.0, 0.0};
   Source<T> s(a, d);
-  if (s.zq) s.ip = 1.0 / of.p, s.iq = 1.0 / of.q;
+  if (s.zq) s.ratio = of.p / of.q;
   typename Source<T>::Columns x;
   s.load(pick * span + (threadIdx.x >> 6) * (int64_t)per * 512 + (threadIdx.x & 63) * 8, x);
   weigh_units(s, x, pick, span, per, weights + (int64_t)b * kMaxUnits);
@@ -726,8 +731,8 @@ static hipError_t verify(const VerifyArgs& a, hipStream_t s) {
     else hipLaunchKernelGGL((verify_stats_kernel<T, 1>), grid, block, 0, s, a, (int)parts, stats);
     if (const hipError_t e = hipGetLastError()) return e;
   }
-  // exact: 512 blocks, as each decides (16 requests of up to 5 + 4 rows of 128256: 25.4 us; 256: 27.5, 1024: 27.0); else 4096 (a full batch of 256 x 128256: 200 us;
-  // 2048: 211, 8192: 203, 16384: 216), and no part below one step; of each block's four waves every one has whole units
+  // exact: 512 blocks, as each decides (16 requests of up to 5 + 4 rows of 128256: 25.4 us; 256: 27.5, 1024: 27.0); else 4096 (256 requests of 6 + 5 rows of 128256: 200 us,
+  // now 189; 2048: 211, 8192: 203, 16384: 216), and no part below one step; of each block's four waves every one has whole units
   const int per = (int)((a.V + 512 * kMaxUnits - 1) / (512 * kMaxUnits));
   const int64_t group = (int64_t)per * kStep, groups = (a.V + group - 1) / group;
   const int64_t wanted = std::min<int64_t>({groups, kMaxPicks, std::max<int64_t>(1, (exact ? 512 : 4096) / a.requests)});
