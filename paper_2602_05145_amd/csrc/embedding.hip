@@ -38,6 +38,38 @@ struct Lane {
       if (TINY ? j < 8 - skip : j >= skip) stf(row, at + j, x[j]);
   }
 };
+// The same as twice four columns, 256 apart, so that every access of a wave to 32-bit numbers is one piece of memory: rows of eight columns on.
+struct Fours {
+  int at[2], skip[2];
+  __device__ __forceinline__ Fours(int first, int lane, int d) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = first + h * 256 + lane * 4;
+      at[h] = min(c, d - 4), skip[h] = min(c - at[h], 4);
+    }
+  }
+  template <bool ONCE = false> __device__ __forceinline__ void load(Loose8<bf16_t>& x, const bf16_t* row) const {
+    const u32x2 lo = fetch<ONCE, u32x2_of_halves>(row + at[0]), hi = fetch<ONCE, u32x2_of_halves>(row + at[1]);
+    x.a = u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+  template <bool ONCE = false> __device__ __forceinline__ void load(Loose8<float>& x, const float* row) const {
+    x.a = fetch<ONCE, f32x4_of_floats>(row + at[0]), x.b = fetch<ONCE, f32x4_of_floats>(row + at[1]);
+  }
+  static __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { put<false, f32x4_of_floats>(p, f32x4{a, b, c, d}); }
+  static __device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) { put<false, u32x2_of_halves>(p, u32x2{f2bf2(a, b), f2bf2(c, d)}); }
+  template <typename T> __device__ __forceinline__ void store(T* row, const float (&x)[8]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (skip[h] == 0) {
+        store4(row + at[h], x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+        continue;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (j >= skip[h]) stf(row, at[h] + j, x[4 * h + j]);
+    }
+  }
+};
 template <typename T> __device__ __forceinline__ void add8(const Loose8<T>& raw, float (&sum)[8]) {
   float x[8];
   raw.get(x);
@@ -46,8 +78,8 @@ template <typename T> __device__ __forceinline__ void add8(const Loose8<T>& raw,
 }
 
 // What a token's sum becomes: its row, or what is added to it.
-template <typename G, bool ADD, bool TINY>
-__device__ __forceinline__ void finish(const Lane<TINY>& own, const float (&sum)[8], const Loose8<G>& old, float scale, G* row) {
+template <typename G, bool ADD, typename L>
+__device__ __forceinline__ void finish(const L& own, const float (&sum)[8], const Loose8<G>& old, float scale, G* row) {
   float x[8];
   if constexpr (ADD) {
     old.get(x);
@@ -271,8 +303,9 @@ __global__ __launch_bounds__(256) void embed_few_kernel(int rows, int vocab, int
 // A wave adds up kCols columns of `piece` rows that follow each other in the order of their tokens.  A token whose rows all lie in the piece is done;
 // of one that goes on in front of or behind it, what lies here is left as a part: parts[2 p] for the first token, parts[2 p + 1] for the last (the first, where there is but
 // one and it goes on in front).  What is added to is requested with the rows, not when their sum is there.  Bound by memory: 32768 rows x 4096 (bf16, to fp32)
-// of as many tokens at 5.3 TB/s, of 1000 tokens (rows in the last cache) at 6.2; added to 11900 rows of the table 144 us, 4.6 TB/s.
-template <typename T, typename G, bool ADD, bool TINY>
+// of as many tokens at 5.3 TB/s, of 1000 tokens (rows in the last cache) at 6.2; added to 11900 rows of the table 144 us, 4.6 TB/s,
+// with eight columns of a lane behind each other, 117 us, 5.6 TB/s, with Fours and, ONCE, rows past the caches that cannot hold them (of 1665 x 2048, which they hold, 0.4 us slower so).
+template <typename T, typename G, bool ADD, bool TINY, bool ONCE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece, int d, int tiles, const uint32_t* __restrict__ sid, const int32_t* __restrict__ pos,
                                                         const T* __restrict__ dy, float scale, G* __restrict__ dtable, float* __restrict__ parts) {
   constexpr int U = ADD ? 4 : 8;
@@ -280,7 +313,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece
   const int64_t p = w / tiles, first = p * piece;
   if (first >= total) return;
   const int lane = threadIdx.x & 63;
-  const Lane<TINY> own((int)(w % tiles) * kCols + lane * 8, d);
+  const int columns = (int)(w % tiles) * kCols;
+  const auto own = [&] {
+    if constexpr (TINY) return Lane<true>(columns + lane * 8, d);
+    else return Fours(columns, lane, d);
+  }();
   const int64_t mine = first + min(lane, piece - 1);   // (total is a multiple of every piece)
   const uint32_t my_id = sid[mine];
   const int my_row = pos[mine];
@@ -297,7 +334,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(int64_t total, int piece
     // (a row without a token, and a sum that is not final, ask for the first row of either: no load stands behind a branch)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      own.load(raw[u], dy + (id[u] == kNone ? (size_t)0 : (size_t)__builtin_amdgcn_readlane(my_row, k0 + u) * d));
+      own.template load<ONCE>(raw[u], dy + (id[u] == kNone ? (size_t)0 : (size_t)__builtin_amdgcn_readlane(my_row, k0 + u) * d));
       if constexpr (ADD) own.load(old[u], dtable + (id[u] != id[u + 1] && id[u] != before ? (size_t)id[u] * d : (size_t)0));
     }
 #pragma unroll
@@ -435,7 +472,8 @@ hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const
   const unsigned blocks = (unsigned)((p.pieces * p.tiles + 3) / 4);
   {
     ProfScope ps("embed_sum", (double)a.rows * a.d, (double)a.rows * a.d * sizeof(T), s);
-    hipLaunchKernelGGL((embed_sum_kernel<T, G, ADD, TINY>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable, parts);
+    const bool once = !TINY && (double)a.rows * a.d * sizeof(T) >= kLastCache;
+    hipLaunchKernelGGL((once ? embed_sum_kernel<T, G, ADD, TINY, !TINY> : embed_sum_kernel<T, G, ADD, TINY, false>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable, parts);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (p.pieces < 2) return hipSuccess;

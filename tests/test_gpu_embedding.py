@@ -161,6 +161,11 @@ def test_gradient_of_one_token_in_most_rows(rows, others):
     check_gradient(ids, "bf16", "fp32", 99, 8, True, repeat=True)
 
 
+@pytest.mark.parametrize("dtype,out,rows,d,off", [("bf16", "fp32", 32768, 4107, 1), ("bf16", "bf16", 32768, 4096, 0), ("fp32", "fp32", 16385, 4101, 2)])
+def test_gradient_of_more_than_the_last_cache(dtype, out, rows, d, off):
+    check_gradient(make_ids(rows, 3001, "holes", 1), dtype, out, 3001, d, True, off=off)
+
+
 @pytest.mark.parametrize("off", [1, 2, 3, 5])
 @pytest.mark.parametrize("dtype,out", [("fp32", "fp32"), ("bf16", "bf16")])
 def test_gradient_of_arrays_that_begin_anywhere(off, dtype, out):
