@@ -473,7 +473,8 @@ hipError_t sums(const EmbedBwdArgs& a, const Plan& p, const uint32_t* sid, const
   {
     ProfScope ps("embed_sum", (double)a.rows * a.d, (double)a.rows * a.d * sizeof(T), s);
     const bool once = !TINY && (double)a.rows * a.d * sizeof(T) >= kLastCache;
-    hipLaunchKernelGGL((once ? embed_sum_kernel<T, G, ADD, TINY, !TINY> : embed_sum_kernel<T, G, ADD, TINY, false>), dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable, parts);
+    const auto kernel = once ? embed_sum_kernel<T, G, ADD, TINY, !TINY> : embed_sum_kernel<T, G, ADD, TINY, false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, s, p.total, p.piece, (int)a.d, p.tiles, sid, pos, (const T*)a.dy, a.scale, (G*)a.dtable, parts);
     if (const hipError_t e = hipGetLastError()) return e;
   }
   if (p.pieces < 2) return hipSuccess;
